@@ -329,6 +329,148 @@ SK_API const char *sinkhorn_status_string(sk_status s);
  */
 SK_API int32_t sinkhorn_regime(const sk_problem *p);
 
+/*
+ * Routed layers: a layer of E experts of which each of T tokens takes k.  With
+ * C = -logits [T, E], uniform mu over the tokens and nu over the experts,
+ * lambda * beta of sinkhorn_forward is the per-expert offset under which the
+ * experts are taken evenly: it is the `bias` of the router below.  The
+ * conventions at the top of this file hold; in addition, indices that another
+ * call of this library wrote (offsets, tokens, slots) are checked by the
+ * kernels: one out of range names no row and no token.
+ */
+typedef enum { SK_F32 = 0, SK_BF16 = 1, SK_F16 = 2 } sk_dtype;
+
+typedef struct {
+    int32_t T;           /* tokens, 0 <= T <= 2^24                                     */
+    int32_t E;           /* experts, 1 <= E <= 1024                                    */
+    int32_t k;           /* experts of a token, 1 <= k <= min(E, 16)                   */
+    int32_t dtype;       /* sk_dtype of logits and grad_logits                         */
+    int32_t renormalize; /* 1: a token's weights are a softmax over its experts alone;
+                            0: they are the softmax over all experts                   */
+} sk_router;
+
+/*
+ * Router, forward.  Token t is live if mask[t] != 0 (or mask is NULL) and some
+ * logit of its row is above -inf; n is the number of live tokens.  A live
+ * token takes the first k experts by descending logits[t, e] + bias[e] (that
+ * sum rounded to 32 bits; ties go to the lowest e; an expert whose sum is -inf
+ * or NaN is not taken); the bias chooses only.  A pair (t, s) that has no
+ * expert has experts = slots = -1 and weight 0.
+ *
+ *   logits   [T, E]  dtype
+ *   bias     [E]     (may be NULL)       mask [T] bytes (may be NULL)
+ *   weights  [T, k]        out  weights of the chosen (see renormalize)
+ *   experts  [T, k] int32  out
+ *   counts   [E]    int32  out  pairs of each expert
+ *   offsets  [E+1]  int32  out  exclusive sums of counts: expert e has the
+ *                               rows offsets[e] <= r < offsets[e+1]
+ *   tokens   [T k]  int32  out  token of each row, rows in the order (expert,
+ *                               token, slot); -1 from row offsets[E] on
+ *   slots    [T, k] int32  out  row of each pair: tokens[slots[t, s]] = t
+ *   balance  [1]           out  E sum_e f_e P_e with f_e = counts[e] / (k n),
+ *                               P_e = mean of softmax(logits)_e over the live
+ *   z_loss   [1]           out  mean of logsumexp(logits_t)^2 over the live
+ *   state    [2 T + 1]     out  for the backward pass
+ * With n = 0 both losses are 0.  A NaN (or +inf) among a live token's logits
+ * makes its weights and the losses NaN; masked tokens' logits are not used.
+ * Deterministic (fixed order, no atomics).
+ */
+SK_API size_t sinkhorn_route_workspace_bytes(const sk_router *r);
+SK_API sk_status sinkhorn_route_forward(const sk_router *r, const void *logits, const float *bias,
+                                        const uint8_t *mask, float *weights, int32_t *experts, int32_t *counts,
+                                        int32_t *offsets, int32_t *tokens, int32_t *slots, float *balance,
+                                        float *z_loss, float *state, void *workspace, size_t ws_bytes,
+                                        void *stream);
+
+/*
+ * Router, backward: grad_logits [T, E] (dtype) of
+ *   sum grad_weights * weights + grad_balance * balance + grad_z * z_loss
+ * (each gradient a device array of its output's shape, or NULL for none).  The
+ * choice of experts and the counts are constants.  0 for tokens not live.
+ */
+SK_API sk_status sinkhorn_route_backward(const sk_router *r, const void *logits, const float *weights,
+                                         const int32_t *experts, const int32_t *counts, const float *state,
+                                         const float *grad_weights, const float *grad_balance, const float *grad_z,
+                                         void *grad_logits, void *stream);
+
+typedef struct {
+    int32_t T;     /* tokens, 0 <= T <= 2^24                               */
+    int32_t k;     /* pairs of a token, 1 <= k <= 16; rows R = T k         */
+    int32_t E;     /* experts, 1 <= E <= 1024                              */
+    int32_t K, N;  /* columns of x and of y, 1 <= K, N <= 2^16, and
+                      E N K, R K, R N <= 2^34                              */
+    int32_t dtype; /* SK_BF16 or SK_F16: type of x, w, y and gradients     */
+} sk_experts;
+
+/*
+ * Experts' products.  Row r, offsets[e] <= r < offsets[e + 1], belongs to
+ * expert e with the matrix w[e] [N, K] (as a linear layer has it):
+ *   y[r, :] = w[e] x[src(r), :],   rows from offsets[E] on: 0,
+ * src(r) = tokens[r] with x [T, K], or r with x [R, K] where tokens is NULL.
+ * offsets, tokens and slots as the router writes them.  16-bit factors, sums
+ * in 32 bits, one rounding to dtype.  Deterministic.
+ */
+SK_API sk_status sinkhorn_experts_forward(const sk_experts *p, const void *x, const void *w,
+                                          const int32_t *offsets, const int32_t *tokens, void *y, void *stream);
+
+/*
+ * Gradient of x: with slots [T, k], grad_x [T, K] = sum_s of the rows
+ * slots[t, s] of grad_y times their expert's matrix, the rows' products kept
+ * in 32 bits in the workspace until they are summed; with slots NULL, grad_x
+ * [R, K] is the rows' own (no workspace).
+ */
+SK_API size_t sinkhorn_experts_workspace_bytes(const sk_experts *p);
+SK_API sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_y, const void *w,
+                                                 const int32_t *offsets, const int32_t *slots, void *grad_x,
+                                                 void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradient of w [E, N, K]: sum_r grad_y[r]^T x[src(r)] over each expert's rows
+ * (0 for an expert without rows). */
+SK_API sk_status sinkhorn_experts_backward_weight(const sk_experts *p, const void *grad_y, const void *x,
+                                                  const int32_t *offsets, const int32_t *tokens, void *grad_w,
+                                                  void *stream);
+
+/*
+ * Dropout from a counter-based generator, on top of a residual:
+ *   y_i = residual_i + scale * x_i  where u_i >= threshold, else residual_i,
+ * i < n <= 2^34 the element's number in row-major order.  u_i are 16 bits of
+ * Philox4x32-10 with key `seed` and counter (i / 8, offset) (64 bits each,
+ * low words first): word (i mod 8) / 2, its low half for even i.  threshold =
+ * round(65536 p), at most 65535; scale = 65536 / (65536 - threshold), so the
+ * rate is p to 16 bits and the mean is kept.  0 <= p < 1 (SK_ERR_ARG).  The
+ * gradient of x is the same call on the gradient of y, without a residual.
+ * x, y and residual (may be NULL) have the type dtype; y may be x or residual.
+ */
+SK_API sk_status sinkhorn_dropout(int64_t n, int32_t dtype, const void *x, const void *residual, void *y, double p,
+                                  uint64_t seed, uint64_t offset, void *stream);
+
+typedef struct {
+    int32_t T;     /* tokens, 0 <= T <= 2^24                             */
+    int32_t D;     /* elements of a row, 1 <= D <= 2^24, T k D <= 2^34   */
+    int32_t k;     /* pairs of a token, 1 <= k <= 16                     */
+    int32_t dtype; /* sk_dtype of z, residual, y and their gradients     */
+} sk_combine;
+
+/*
+ * Combination of expert rows with dropout (as above over y, p = 0: none):
+ *   y[t] = residual[t] + scale keep sum_s weights[t, s] z[slots[t, s]],
+ * z [T k, D], weights [T, k], slots [T, k] as from the router (pairs with slot
+ * -1 add nothing), residual [T, D] or NULL, y [T, D].
+ */
+SK_API sk_status sinkhorn_combine_forward(const sk_combine *c, const void *z, const float *weights,
+                                          const int32_t *slots, const void *residual, void *y, double p,
+                                          uint64_t seed, uint64_t offset, void *stream);
+
+/*
+ * Its gradients: grad_z [T k, D] (0 in the rows from *used_rows on, which no
+ * slot names: used_rows is the router's offsets + E, a device pointer) and
+ * grad_weights [T, k] (0 for pairs without a row); the residual's is grad_y.
+ */
+SK_API sk_status sinkhorn_combine_backward(const sk_combine *c, const void *z, const float *weights,
+                                           const int32_t *slots, const int32_t *used_rows, const void *grad_y,
+                                           void *grad_z, float *grad_weights, double p, uint64_t seed,
+                                           uint64_t offset, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,20 @@ from ._binding import (  # noqa: F401
     sinkhorn_workspace_bytes,
 )
 from .loss import SinkhornLoss, SinkhornPointsLoss, sinkhorn_loss, sinkhorn_loss_points  # noqa: F401
+from .routed import (  # noqa: F401
+    Routing,
+    sinkhorn_combine_backward,
+    sinkhorn_combine_forward,
+    sinkhorn_dropout,
+    sinkhorn_expert_combine,
+    sinkhorn_expert_product,
+    sinkhorn_experts_backward_input,
+    sinkhorn_experts_backward_weight,
+    sinkhorn_experts_forward,
+    sinkhorn_route,
+    sinkhorn_route_backward,
+    sinkhorn_route_forward,
+)
 
 __all__ = [
     "NOALLOC_SCRATCH_BYTES",
@@ -52,4 +66,16 @@ __all__ = [
     "sinkhorn_sharp_workspace_bytes",
     "sinkhorn_status_string",
     "sinkhorn_workspace_bytes",
+    "Routing",
+    "sinkhorn_combine_backward",
+    "sinkhorn_combine_forward",
+    "sinkhorn_dropout",
+    "sinkhorn_expert_combine",
+    "sinkhorn_expert_product",
+    "sinkhorn_experts_backward_input",
+    "sinkhorn_experts_backward_weight",
+    "sinkhorn_experts_forward",
+    "sinkhorn_route",
+    "sinkhorn_route_backward",
+    "sinkhorn_route_forward",
 ]

@@ -40,6 +40,16 @@ EXPORTED = (
     "sinkhorn_sharp_workspace_bytes",
     "sinkhorn_describe",
     "sinkhorn_forward_warm",
+    "sinkhorn_route_workspace_bytes",
+    "sinkhorn_route_forward",
+    "sinkhorn_route_backward",
+    "sinkhorn_experts_forward",
+    "sinkhorn_experts_workspace_bytes",
+    "sinkhorn_experts_backward_input",
+    "sinkhorn_experts_backward_weight",
+    "sinkhorn_dropout",
+    "sinkhorn_combine_forward",
+    "sinkhorn_combine_backward",
 )
 
 
@@ -59,6 +69,18 @@ class SkProblem(ctypes.Structure):
         ("n_iter", ctypes.c_int32),
         ("tol", ctypes.c_float),
     ]
+
+
+class SkRouter(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "E", "k", "dtype", "renormalize")]
+
+
+class SkExperts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "K", "N", "dtype")]
+
+
+class SkCombine(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "D", "k", "dtype")]
 
 
 def library_path() -> str:
@@ -106,6 +128,23 @@ def load_library():
     lib.sinkhorn_forward_warm.restype = ctypes.c_int
     lib.sinkhorn_describe.argtypes = [PP, I, ctypes.c_char_p, ctypes.c_size_t]
     lib.sinkhorn_describe.restype = ctypes.c_int32
+    Z, U, D = ctypes.c_size_t, ctypes.c_uint64, ctypes.c_double
+    PR, PE, PC = ctypes.POINTER(SkRouter), ctypes.POINTER(SkExperts), ctypes.POINTER(SkCombine)
+    lib.sinkhorn_route_workspace_bytes.argtypes = [PR]
+    lib.sinkhorn_route_workspace_bytes.restype = Z
+    lib.sinkhorn_route_forward.argtypes = [PR, P, P, P, P, P, P, P, P, P, P, P, P, P, Z, P]
+    lib.sinkhorn_route_backward.argtypes = [PR, P, P, P, P, P, P, P, P, P, P]
+    lib.sinkhorn_experts_forward.argtypes = [PE, P, P, P, P, P, P]
+    lib.sinkhorn_experts_workspace_bytes.argtypes = [PE]
+    lib.sinkhorn_experts_workspace_bytes.restype = Z
+    lib.sinkhorn_experts_backward_input.argtypes = [PE, P, P, P, P, P, P, Z, P]
+    lib.sinkhorn_experts_backward_weight.argtypes = [PE, P, P, P, P, P, P]
+    lib.sinkhorn_dropout.argtypes = [ctypes.c_int64, I, P, P, P, D, U, U, P]
+    lib.sinkhorn_combine_forward.argtypes = [PC, P, P, P, P, P, D, U, U, P]
+    lib.sinkhorn_combine_backward.argtypes = [PC, P, P, P, P, P, P, P, D, U, U, P]
+    for name in ("route_forward", "route_backward", "experts_forward", "experts_backward_input",
+                 "experts_backward_weight", "dropout", "combine_forward", "combine_backward"):
+        getattr(lib, "sinkhorn_" + name).restype = ctypes.c_int
     _lib = lib
     return lib
 

@@ -1,0 +1,586 @@
+// sk_route.hip -- the router: experts of each token, their weights, counts per expert, the balance and z losses, and
+// the order of the (token, slot) pairs by expert; and the gradient of the logits.
+//
+// A token's logits are held by a group of L lanes, V consecutive ones to a lane (E <= L V), so one read serves the
+// softmax, the k largest and the sums over tokens.  A group takes a run of consecutive tokens and keeps, in the
+// registers of the lane that holds an expert, how many pairs the expert has so far: that count is a pair's rank among
+// the run's pairs of that expert, so the order by (expert, token, slot) needs no sort and no atomics:
+//   sk_route_tokens   one work-group per block of tokens; ranks within the block; counts, probability sums per block
+//   sk_route_scan     per expert, the blocks' counts summed into starts; totals
+//   sk_route_place    start of the expert + start of the block + rank; the losses
+// Few tokens are one block, which finishes in the first launch.  All sums are taken in a fixed order in 32 bits.
+#include <type_traits>
+
+#include "sk_routed.h"
+
+namespace sk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxK = 16;
+constexpr int kMaxRun = 32;        // tokens of a group: ranks within a run stay below 2^16 and the pairs in LDS
+constexpr int kBlocksWanted = 512;  // two work-groups per CU
+constexpr int kScanCols = 16;
+
+// Reductions over aligned groups of L lanes; every lane of the group ends with the same bits.
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+    v = sum_q(v);
+    if constexpr (L >= 16) v += dpp<kRowRor8>(v);
+    if constexpr (L >= 32) {
+        const LanePair a = swap16(v);
+        v = a.lo + a.hi;
+    }
+    if constexpr (L >= 64) {
+        const LanePair b = swap32(v);
+        v = b.lo + b.hi;
+    }
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+    v = max_q(v);
+    if constexpr (L >= 16) v = fmaxf(v, dpp<kRowRor8>(v));
+    if constexpr (L >= 32) {
+        const LanePair a = swap16(v);
+        v = fmaxf(a.lo, a.hi);
+    }
+    if constexpr (L >= 64) {
+        const LanePair b = swap32(v);
+        v = fmaxf(b.lo, b.hi);
+    }
+    return v;
+}
+// The group's bits of a wavefront's ballot.
+template <int L>
+__device__ __forceinline__ uint64_t group_ballot(bool b) {
+    const uint64_t all = __builtin_amdgcn_ballot_w64(b);
+    if constexpr (L == 64) return all;
+    return (all >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << (L & 63)) - 1);
+}
+
+// This lane's V logits of token t; -inf past the last expert.
+template <class T, int L, int V, bool VEC>
+__device__ __forceinline__ void load_logits(const T *row, int E, int first, float (&x)[V]) {
+    if constexpr (VEC) {
+        static_assert(V == 4, "vector loads are of four logits");
+        if (first < E) {  // E is a multiple of four
+            if constexpr (sizeof(T) == 4) {
+                const float4 a = *reinterpret_cast<const float4 *>(row + first);
+                x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+            } else {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                const T4 a = *reinterpret_cast<const T4 *>(row + first);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) x[v] = (float)a[v];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = neg_inf();
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = first + v < E ? (float)row[first + v] : neg_inf();
+    }
+}
+
+struct RoutePlan {
+    int run;     // tokens of a group
+    int groups;  // groups of a work-group
+    int blocks;  // work-groups
+};
+
+// Workspace: counts [blocks][E], probability sums [blocks][E], z sums [blocks], live tokens [blocks]; totals of the
+// probability sums [E], of z and of the live tokens.
+struct RouteSpace {
+    int32_t *cnt;
+    float *prob, *z, *live, *prob_all, *z_all, *live_all;
+};
+__host__ __device__ inline RouteSpace route_space(void *ws, int blocks, int E) {
+    RouteSpace s;
+    s.cnt = static_cast<int32_t *>(ws);
+    s.prob = reinterpret_cast<float *>(s.cnt + (size_t)blocks * E);
+    s.z = s.prob + (size_t)blocks * E;
+    s.live = s.z + blocks;
+    s.prob_all = s.live + blocks;
+    s.z_all = s.prob_all + E;
+    s.live_all = s.z_all + 1;
+    return s;
+}
+
+// Exclusive sums over E experts of counts read through `count`, by the whole work-group, into off[0..E] (LDS).
+template <class Count>
+__device__ __forceinline__ void expert_offsets(int E, int32_t *off, int32_t *wave_total, Count count) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int32_t base = 0;
+    for (int e0 = 0; e0 < E; e0 += kThreads) {
+        const int e = e0 + threadIdx.x;
+        const int32_t c = e < E ? count(e) : 0;
+        int32_t sum = c;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t up = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += up;
+        }
+        if (lane == 63) wave_total[w] = sum;
+        __syncthreads();
+        int32_t before = base;
+        for (int q = 0; q < w; ++q) before += wave_total[q];
+        if (e < E) off[e] = before + sum - c;
+        for (int q = 0; q < kThreads / 64; ++q) base += wave_total[q];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) off[E] = base;
+    __syncthreads();
+}
+
+// The losses from the totals, by one work-group: balance = E sum_e f_e P_e, z.
+template <class Count, class Prob>
+__device__ __forceinline__ void route_losses(const RouteArgs &A, float live, float z, float *red, Count count,
+                                             Prob prob) {
+    const float n = fmaxf(live, 1.f);
+    float s = 0.f;
+    for (int e = threadIdx.x; e < A.E; e += kThreads) s += ((float)count(e) / ((float)A.k * n)) * (prob(e) / n);
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float all = 0.f;
+        for (int q = 0; q < kThreads / 64; ++q) all += red[q];
+        *A.balance = (float)A.E * all;
+        *A.z_loss = z / n;
+        A.state[2 * (size_t)A.T] = live;
+    }
+}
+
+// ONE: the only work-group; writes the order and the losses too.
+template <class T, int L, int V, bool VEC, bool ONE>
+__global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePlan P) {
+    constexpr int G = kThreads / L;
+    extern __shared__ int32_t lds[];
+    int32_t *cnt_lds = lds;                                      // [G][L V]
+    float *prob_lds = reinterpret_cast<float *>(lds + G * L * V);  // [G][L V]
+    uint32_t *pair = reinterpret_cast<uint32_t *>(prob_lds + G * L * V);  // [G][run][k]: expert << 16 | rank
+    __shared__ float z_lds[G], live_lds[G], red[kThreads / 64];
+    __shared__ int32_t off[ONE ? L * V + 1 : 1], wave_total[kThreads / 64];
+
+    const int E = A.E, k = A.k;
+    const int lane = threadIdx.x & (L - 1), g = threadIdx.x / L;
+    const int first = lane * V;
+    const int64_t t0 = ((int64_t)blockIdx.x * G + g) * P.run;
+    uint32_t *mine = pair + (size_t)g * P.run * k;
+
+    float bias[V], psum[V];
+    int32_t cnt[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bias[v] = A.bias && first + v < E ? A.bias[first + v] : 0.f;
+        psum[v] = 0.f;
+        cnt[v] = 0;
+    }
+    float zsum = 0.f, nlive = 0.f;
+
+    for (int q = 0; q < P.run; ++q) {
+        const int64_t t = t0 + q;
+        const bool here = t < A.T;  // one answer for the group; the wavefront's groups stay together
+        float x[V];
+        load_logits<T, L, V, VEC>(static_cast<const T *>(A.logits) + (here ? t : 0) * (int64_t)E, E,
+                                  here ? first : E, x);
+        bool live = here && (!A.mask || A.mask[t]);
+
+        // softmax: the largest logit, the sum of exponentials
+        float mx = x[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) mx = fmaxf(mx, x[v]);
+        mx = group_max<L>(mx);
+        if (__builtin_amdgcn_ballot_w64(live && mx == neg_inf())) {
+            // Nothing above -inf: no row, unless a NaN is in it (fmaxf passes over NaN), which then shows in the row.
+            bool nan = false;
+#pragma unroll
+            for (int v = 0; v < V; ++v) nan |= x[v] != x[v];
+            nan = group_ballot<L>(nan) != 0;
+            if (mx == neg_inf()) {
+                if (nan) mx = __builtin_nanf("");
+                else live = false;
+            }
+        }
+        float ex[V], sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            ex[v] = first + v < E ? ex2((x[v] - mx) * kLog2e) : 0.f;
+            sum += ex[v];
+        }
+        sum = group_sum<L>(sum);
+        if (live) {
+            const float inv = 1.f / sum;
+#pragma unroll
+            for (int v = 0; v < V; ++v) psum[v] += ex[v] * inv;
+            const float lse = mx + lg2(sum) * kLn2;
+            zsum += lse * lse;
+            nlive += 1.f;
+        }
+        if (here && lane == 0) {
+            A.state[2 * t] = live ? mx : neg_inf();
+            A.state[2 * t + 1] = sum;
+        }
+
+        // the k largest scores, ties to the lowest expert; scores of -inf and NaN are not taken
+        float sc[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float s = x[v] + bias[v];
+            sc[v] = live && first + v < E && s > neg_inf() ? s : neg_inf();
+        }
+        int my_expert = -1;
+        float my_logit = neg_inf();
+        uint32_t my_pair = 0xFFFFFFFFu;
+        for (int s = 0; s < k; ++s) {
+            float m = sc[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) m = fmaxf(m, sc[v]);
+            const float best = group_max<L>(m);
+            const bool some = best > neg_inf();
+            const int owner = some ? __builtin_ctzll(group_ballot<L>(m == best)) : 0;
+            uint32_t word = 0;
+            float logit = 0.f;
+            bool open = some && lane == owner;  // the owner's first score equal to the best is the one
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool hit = open && sc[v] == best;
+                word = hit ? (uint32_t)(first + v) << 16 | (uint32_t)cnt[v] : word;
+                logit = hit ? x[v] : logit;
+                cnt[v] += hit;
+                sc[v] = hit ? neg_inf() : sc[v];
+                open = open && !hit;
+            }
+            word = __shfl((int)word, owner, L);
+            logit = __shfl(logit, owner, L);
+            if (lane == s && some) {
+                my_expert = (int)(word >> 16);
+                my_logit = logit;
+                my_pair = word;
+            }
+        }
+
+        // weights of the chosen: lane s has slot s
+        float w = 0.f;
+        if (A.renormalize) {
+            const float top = group_max<L>(my_logit);
+            // A chosen logit that is not finite shows in the weights, as in any softmax.
+            const float u = my_expert >= 0 ? ex2((my_logit - top) * kLog2e) : 0.f;
+            const float all = group_sum<L>(u);
+            // The row's own sum is used for NaN alone: a NaN logit is never chosen, and its row must not look sound.
+            w = my_expert >= 0 ? (sum != sum ? sum : u / all) : 0.f;
+        } else {
+            w = my_expert >= 0 ? ex2((my_logit - mx) * kLog2e) / sum : 0.f;
+        }
+        if (here && lane < k) {
+            A.weights[t * k + lane] = w;
+            A.experts[t * k + lane] = my_expert;
+            mine[q * k + lane] = my_pair;
+        }
+    }
+
+    // The block's totals, and each group's start among them.
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        cnt_lds[g * L * V + first + v] = cnt[v];
+        prob_lds[g * L * V + first + v] = psum[v];
+    }
+    if (lane == 0) z_lds[g] = zsum, live_lds[g] = nlive;
+    __syncthreads();
+    const RouteSpace S = route_space(A.ws, P.blocks, E);
+    for (int e = threadIdx.x; e < E; e += kThreads) {
+        int32_t c = 0;
+        float p = 0.f;
+        for (int q = 0; q < G; ++q) {
+            const int32_t n = cnt_lds[q * L * V + e];
+            cnt_lds[q * L * V + e] = c;
+            c += n;
+            p += prob_lds[q * L * V + e];
+        }
+        if constexpr (ONE) {
+            A.counts[e] = c;
+            prob_lds[e] = p;  // the totals take the places of groups 0 and 1, which this thread alone has read
+            reinterpret_cast<int32_t *>(prob_lds)[L * V + e] = c;
+        } else {
+            S.cnt[(size_t)blockIdx.x * E + e] = c;
+            S.prob[(size_t)blockIdx.x * E + e] = p;
+        }
+    }
+    float z = 0.f, live = 0.f;
+    for (int q = 0; q < G; ++q) z += z_lds[q], live += live_lds[q];
+    __syncthreads();
+    if constexpr (ONE) {
+        const int32_t *total = reinterpret_cast<const int32_t *>(prob_lds) + L * V;
+        expert_offsets(E, off, wave_total, [&](int e) { return total[e]; });
+        for (int e = threadIdx.x; e <= E; e += kThreads) A.offsets[e] = off[e];
+        route_losses(A, live, z, red, [&](int e) { return total[e]; }, [&](int e) { return prob_lds[e]; });
+    } else if (threadIdx.x == 0) {
+        S.z[blockIdx.x] = z;
+        S.live[blockIdx.x] = live;
+    }
+
+    for (int q = lane; q < P.run * k; q += L) {
+        const int64_t at = t0 * k + q;
+        if (at >= (int64_t)A.T * k) break;
+        const uint32_t word = mine[q];
+        int32_t slot = -1;
+        if (word != 0xFFFFFFFFu) {
+            const int e = (int)(word >> 16);
+            slot = cnt_lds[g * L * V + e] + (int32_t)(word & 0xFFFFu);
+            if constexpr (ONE) {
+                slot += off[e];
+                A.tokens[slot] = (int32_t)(t0 + q / k);
+            }
+        }
+        A.slots[at] = slot;  // !ONE: the rank within the block until sk_route_place
+    }
+    if constexpr (ONE)
+        for (int64_t r = off[E] + threadIdx.x; r < (int64_t)A.T * k; r += kThreads) A.tokens[r] = -1;
+}
+
+// Work-groups of kScanCols experts: the blocks' counts become starts, in place; totals of counts and probabilities.
+// The last work-group sums z and the live tokens.
+__global__ __launch_bounds__(kThreads) void sk_route_scan(RouteArgs A, RoutePlan P) {
+    constexpr int N = kThreads / kScanCols;  // strands of a column
+    __shared__ int32_t c_lds[N][kScanCols];
+    __shared__ float p_lds[N][kScanCols];
+    __shared__ float red[2][kThreads / 64];
+    const RouteSpace S = route_space(A.ws, P.blocks, A.E);
+    if (blockIdx.x + 1 == gridDim.x) {
+        float z = 0.f, n = 0.f;
+        for (int b = threadIdx.x; b < P.blocks; b += kThreads) z += S.z[b], n += S.live[b];
+        z = wave_sum(z), n = wave_sum(n);
+        if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = z, red[1][threadIdx.x >> 6] = n;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int q = 1; q < kThreads / 64; ++q) z += red[0][q], n += red[1][q];
+            *S.z_all = z;
+            *S.live_all = n;
+        }
+        return;
+    }
+    const int col = threadIdx.x % kScanCols, strand = threadIdx.x / kScanCols;
+    const int e = blockIdx.x * kScanCols + col;
+    const int per = (P.blocks + N - 1) / N;
+    const int b0 = min(strand * per, P.blocks), b1 = min(b0 + per, P.blocks);
+    int32_t c = 0;
+    float p = 0.f;
+    if (e < A.E)
+        for (int b = b0; b < b1; ++b) {
+            c += S.cnt[(size_t)b * A.E + e];
+            p += S.prob[(size_t)b * A.E + e];
+        }
+    c_lds[strand][col] = c;
+    p_lds[strand][col] = p;
+    __syncthreads();
+    if (e >= A.E) return;
+    int32_t start = 0;
+    for (int q = 0; q < strand; ++q) start += c_lds[q][col];
+    if (strand == 0) {
+        for (int q = 1; q < N; ++q) c += c_lds[q][col], p += p_lds[q][col];
+        A.counts[e] = c;
+        S.prob_all[e] = p;
+    }
+    for (int b = b0; b < b1; ++b) {
+        int32_t *at = S.cnt + (size_t)b * A.E + e;
+        const int32_t n = *at;
+        *at = start;
+        start += n;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void sk_route_place(RouteArgs A, RoutePlan P) {
+    extern __shared__ int32_t off[];  // [E + 1]
+    __shared__ int32_t wave_total[kThreads / 64];
+    __shared__ float red[kThreads / 64];
+    const RouteSpace S = route_space(A.ws, P.blocks, A.E);
+    expert_offsets(A.E, off, wave_total, [&](int e) { return A.counts[e]; });
+    if (blockIdx.x == 0) {
+        for (int e = threadIdx.x; e <= A.E; e += kThreads) A.offsets[e] = off[e];
+        route_losses(A, *S.live_all, *S.z_all, red, [&](int e) { return A.counts[e]; },
+                     [&](int e) { return S.prob_all[e]; });
+    }
+    const int64_t pairs = (int64_t)A.T * A.k, stride = (int64_t)gridDim.x * kThreads;
+    const int tokens_of_block = P.groups * P.run;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < pairs; i += stride) {
+        const int32_t e = A.experts[i];
+        if (e >= 0) {
+            const int32_t t = (int32_t)(i / A.k);
+            const int32_t slot = off[e] + S.cnt[(size_t)(t / tokens_of_block) * A.E + e] + A.slots[i];
+            A.slots[i] = slot;
+            A.tokens[slot] = t;
+        }
+        if (i >= off[A.E]) A.tokens[i] = -1;
+    }
+}
+
+// dl_e = p_e (c_e - sum p c + 2 g_z lse / n) + the weights' part at the chosen, c_e = g_balance E f_e / n.
+template <class T, int L, int V, bool VEC>
+__global__ __launch_bounds__(kThreads) void sk_route_bwd(RouteBwdArgs A) {
+    constexpr int G = kThreads / L;
+    const int E = A.E, k = A.k;
+    const int lane = threadIdx.x & (L - 1), g = threadIdx.x / L;
+    const int first = lane * V;
+    const float n = fmaxf(A.state[2 * (size_t)A.T], 1.f);
+    const float gb = A.g_balance ? *A.g_balance : 0.f, gz = A.g_z ? *A.g_z : 0.f;
+    float coef[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        coef[v] = first + v < E ? gb * (float)E * ((float)A.counts[first + v] / ((float)k * n)) / n : 0.f;
+
+    for (int64_t t0 = (int64_t)blockIdx.x * G; t0 < A.T; t0 += (int64_t)gridDim.x * G) {
+        const int64_t t = t0 + g;
+        const bool here = t < A.T;
+        const int64_t tt = here ? t : t0;
+        float x[V];
+        load_logits<T, L, V, VEC>(static_cast<const T *>(A.logits) + tt * E, E, first, x);
+        const float mx = A.state[2 * tt], sum = A.state[2 * tt + 1];
+        const bool live = mx != neg_inf();
+        const float inv = 1.f / sum, lse = mx + lg2(sum) * kLn2;
+        float p[V], pc = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            p[v] = first + v < E ? ex2((x[v] - mx) * kLog2e) * inv : 0.f;
+            pc = __builtin_fmaf(p[v], coef[v], pc);
+        }
+        pc = group_sum<L>(pc);
+        // lane s has slot s
+        float w = 0.f, gw = 0.f;
+        int expert = -1;
+        if (A.g_weights && lane < k) {
+            expert = A.experts[tt * k + lane];
+            w = A.weights[tt * k + lane];
+            gw = A.g_weights[tt * k + lane];
+            if (expert < 0) w = gw = 0.f;
+        }
+        const float wg = group_sum<L>(w * gw);
+        const float all = 2.f * gz * lse / n - pc - (A.renormalize ? 0.f : wg);
+        const float own = A.renormalize ? w * (gw - wg) : w * gw;
+        float d[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) d[v] = p[v] * (coef[v] + all);
+        if (A.g_weights) {
+            for (int s = 0; s < k; ++s) {
+                const int e = __shfl(expert, s, L);
+                const float add = __shfl(own, s, L);
+#pragma unroll
+                for (int v = 0; v < V; ++v) d[v] += e == first + v ? add : 0.f;
+            }
+        }
+        if (!here) continue;
+        T *out = static_cast<T *>(A.g_logits) + t * E;
+#pragma unroll
+        for (int v = 0; v < V; ++v) d[v] = live ? d[v] : 0.f;
+        if constexpr (VEC) {
+            if (first < E) {
+                if constexpr (sizeof(T) == 4) {
+                    *reinterpret_cast<float4 *>(out + first) = make_float4(d[0], d[1], d[2], d[3]);
+                } else {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    T4 o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[v] = (T)d[v];
+                    *reinterpret_cast<T4 *>(out + first) = o;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (first + v < E) out[first + v] = (T)d[v];
+        }
+    }
+}
+
+// Lanes of a group: as few as hold the experts at four (beyond 256 experts: up to 16) to a lane, so that small rows
+// share a wavefront, but not fewer than 16, which carry the k <= 16 slots (eight for up to eight experts).
+int group_lanes(int E) { return E <= 8 ? 8 : E <= 64 ? 16 : E <= 128 ? 32 : 64; }
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// Calls f(L, V, vector loads) for the shape that holds E experts.
+template <class F>
+hipError_t with_shape(int E, bool vec, F f) {
+    if (E <= 8) return f(Int<8>{}, Int<1>{}, std::false_type{});
+    if (E <= 16) return f(Int<16>{}, Int<1>{}, std::false_type{});
+    if (E <= 64) return vec ? f(Int<16>{}, Int<4>{}, std::true_type{}) : f(Int<16>{}, Int<4>{}, std::false_type{});
+    if (E <= 128) return vec ? f(Int<32>{}, Int<4>{}, std::true_type{}) : f(Int<32>{}, Int<4>{}, std::false_type{});
+    if (E <= 256) return vec ? f(Int<64>{}, Int<4>{}, std::true_type{}) : f(Int<64>{}, Int<4>{}, std::false_type{});
+    if (E <= 512) return f(Int<64>{}, Int<8>{}, std::false_type{});
+    return f(Int<64>{}, Int<16>{}, std::false_type{});
+}
+
+// One block while each group has at most four tokens: two more launches take longer than those in turn.
+RoutePlan route_plan(int T, int E) {
+    RoutePlan P;
+    P.groups = kThreads / group_lanes(E);
+    if (T <= 4 * P.groups) {
+        P.run = T > 0 ? (T + P.groups - 1) / P.groups : 1;
+        P.blocks = 1;
+        return P;
+    }
+    const int64_t wanted = (int64_t)kBlocksWanted * P.groups;
+    int64_t run = (T + wanted - 1) / wanted;
+    P.run = (int)(run > kMaxRun ? kMaxRun : run);
+    const int per = P.groups * P.run;
+    P.blocks = (int)(((int64_t)T + per - 1) / per);
+    return P;
+}
+
+bool vector_rows(const void *p, int E, int dtype) {
+    return E % 4 == 0 && ((uintptr_t)p % (dtype == SK_F32 ? 16 : 8)) == 0;
+}
+
+}  // namespace
+
+size_t route_workspace_bytes(int T, int E, int k) {
+    (void)k;
+    const RoutePlan P = route_plan(T, E);
+    if (P.blocks == 1) return 0;
+    return ((size_t)P.blocks * E * 2 + (size_t)P.blocks * 2 + E + 2) * 4;
+}
+
+hipError_t launch_route_forward(const RouteArgs &a, hipStream_t st) {
+    const RoutePlan P = route_plan(a.T, a.E);
+    hipError_t err = with_type(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        return with_shape(a.E, vector_rows(a.logits, a.E, a.dtype), [&](auto l, auto v, auto vec) {
+            constexpr int L = decltype(l)::value, V = decltype(v)::value;
+            constexpr bool VEC = decltype(vec)::value;
+            const size_t lds = (size_t)(kThreads / L) * (2 * L * V + (size_t)P.run * a.k) * 4;
+            if (P.blocks == 1)
+                hipLaunchKernelGGL((sk_route_tokens<T, L, V, VEC, true>), dim3(1), dim3(kThreads), lds, st, a, P);
+            else
+                hipLaunchKernelGGL((sk_route_tokens<T, L, V, VEC, false>), dim3(P.blocks), dim3(kThreads), lds, st, a,
+                                   P);
+            return hipGetLastError();
+        });
+    });
+    if (err != hipSuccess || P.blocks == 1) return err;
+    hipLaunchKernelGGL(sk_route_scan, dim3((a.E + kScanCols - 1) / kScanCols + 1), dim3(kThreads), 0, st, a, P);
+    const int64_t pairs = (int64_t)a.T * a.k;
+    int64_t grid = (pairs + 4 * kThreads - 1) / (4 * kThreads);
+    if (grid > 1024) grid = 1024;
+    hipLaunchKernelGGL(sk_route_place, dim3((unsigned)grid), dim3(kThreads), ((size_t)a.E + 1) * 4, st, a, P);
+    return hipGetLastError();
+}
+
+hipError_t launch_route_backward(const RouteBwdArgs &a, hipStream_t st) {
+    if (a.T == 0) return hipSuccess;
+    const int G = kThreads / group_lanes(a.E);
+    int64_t grid = ((int64_t)a.T + G - 1) / G;
+    if (grid > 2048) grid = 2048;
+    return with_type(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        const bool vec = vector_rows(a.logits, a.E, a.dtype) && vector_rows(a.g_logits, a.E, a.dtype);
+        return with_shape(a.E, vec, [&](auto l, auto v, auto ve) {
+            hipLaunchKernelGGL((sk_route_bwd<T, decltype(l)::value, decltype(v)::value, decltype(ve)::value>),
+                               dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+            return hipGetLastError();
+        });
+    });
+}
+
+}  // namespace sk
