@@ -37,37 +37,69 @@ __device__ __forceinline__ RowRange expert_rows(const ExpertArgs &A, int e) {
     return r;
 }
 
-// The expert and the rows of the id-th tile of up to `tile` rows, tiles counted over the experts in order (E: the
-// rows of none); expert = -1 past the last.  Every lane of the wavefront calls it and gets the answer.
-struct RowTile {
-    int expert, begin, end;
+// Work-groups go round the eight XCDs in turn; each XCD has its own L2.  This gives XCD b % 8 a run of consecutive
+// tiles, so that neighbours share what they read; -1: no tile for this work-group (a grid of a multiple of eight that
+// has at least `tiles`).
+__device__ __forceinline__ int xcd_order(int b, int tiles) {
+    const int run = (tiles + 7) / 8, t = (b & 7) * run + (b >> 3);
+    return (b >> 3) < run && t < tiles ? t : -1;
+}
+
+// The tile of work-group b: up to `tile` rows of an expert (E: the rows of none), and one of `columns` column tiles.
+// Tiles are counted over the experts in order, within an expert by groups of four row tiles that go over the columns
+// together.  How many there are is known here alone, from the offsets.  expert = -1: none.  Every lane of the
+// wavefront calls it and gets the answer.
+struct Tile {
+    int expert, begin, end, column;
 };
-__device__ __forceinline__ RowTile find_row_tile(const ExpertArgs &A, int tile, int id) {
+__device__ __forceinline__ Tile find_tile(const ExpertArgs &A, int tile, int columns, int b) {
     const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int e0 = 0; e0 <= A.E; e0 += 64) {
-        const int e = e0 + lane;
-        RowRange r = {0, 0};
-        if (e <= A.E) r = expert_rows(A, e);
-        const int n = (r.end - r.begin + tile - 1) / tile;
-        int upto = n;
+    const auto row_tiles = [&](RowRange r) { return (r.end - r.begin + tile - 1) / tile; };
+    const RowRange none = expert_rows(A, A.E);
+    int in_experts = 0;
+    for (int e0 = 0; e0 < A.E; e0 += 64) {
+        int n = e0 + lane < A.E ? row_tiles(expert_rows(A, e0 + lane)) : 0;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += up;
-        }
-        upto += before;
-        const bool mine = id < upto && id >= upto - n;
-        const uint64_t who = __builtin_amdgcn_ballot_w64(mine);
-        if (who) {
-            const int q = __builtin_ctzll(who);
-            const int begin = __builtin_amdgcn_readlane(r.begin + (id - (upto - n)) * tile, q);
-            const int end = __builtin_amdgcn_readlane(r.end, q);
-            return {e0 + q, begin, min(begin + tile, end)};
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
+        for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d, 64);
+        in_experts += n;
     }
-    return {-1, 0, 0};
+    in_experts = __builtin_amdgcn_readfirstlane(in_experts);
+    const int t = xcd_order(b, (in_experts + row_tiles(none)) * columns);
+    if (t < 0) return {-1, 0, 0, 0};
+    const int row = t / columns;
+    RowRange r = none;
+    int expert = A.E, before = in_experts;
+    if (row < in_experts) {
+        before = 0;
+        for (int e0 = 0; e0 < A.E; e0 += 64) {
+            RowRange mine = {0, 0};
+            if (e0 + lane < A.E) mine = expert_rows(A, e0 + lane);
+            const int n = row_tiles(mine);
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += up;
+            }
+            upto += before;
+            const uint64_t who = __builtin_amdgcn_ballot_w64(row < upto && row >= upto - n);
+            if (who) {
+                const int q = __builtin_ctzll(who);
+                expert = e0 + q;
+                before = __builtin_amdgcn_readlane(upto - n, q);
+                r.begin = __builtin_amdgcn_readlane(mine.begin, q);
+                r.end = __builtin_amdgcn_readlane(mine.end, q);
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (expert == A.E) return {-1, 0, 0, 0};
+    }
+    const int i = t - before * columns, n = row_tiles(r);
+    const int group = i / (4 * columns), j = i - group * 4 * columns;
+    const int high = min(4, n - group * 4);
+    const int begin = r.begin + (group * 4 + j % high) * tile;
+    return {expert, begin, min(begin + tile, r.end), j / high};
 }
 
 }  // namespace sk

@@ -23,6 +23,244 @@ __device__ __forceinline__ f32x4 mfma16(const Frag8<T> &a, const Frag8<T> &b, f3
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// ---- tiles: columns in whole chunks of eight, every pointer aligned to 16 bytes ----
+//
+// A work-group computes BM x BN results; its wavefronts, WM x WN of them, a part of BM / WM x BN / WN each, held in
+// registers.  The contraction goes in steps of 64.  Both operands' steps are copied to LDS by the memory pipe itself
+// (16 bytes a lane), one step ahead of the products, into one of two buffers; one barrier a step.
+//
+// An operand whose rows run along the contraction ("along": x, w in forward, gy in input) lies in LDS as rows of 64,
+// and a lane's eight elements are one 16-byte read.  An operand whose rows run across it ("across": w in input, gy
+// and x in weight) lies as 64 rows of the tile's width and is read through the transposing LDS read, so no copy is
+// transposed in memory.  LDS takes a copy in lane order, so the places that keep the reads off each other's banks are
+// reached by permuting the lanes' sources: chunk c of row r lies at c ^ (r & 7) ("along", 16-byte chunks), granule q
+// of row d at q ^ spread(d) ("across", 32-byte granules).
+//
+// Elements past the end of the contraction come from a page of zeros; rows and columns past the tile's end repeat the
+// last one and are not stored.
+
+constexpr int kDeep = 64;
+
+__device__ __attribute__((aligned(16))) uint32_t zero_page[4];
+
+using GlobalWord = const __attribute__((address_space(1))) uint32_t;
+using LdsWord = __attribute__((address_space(3))) uint32_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+using LdsShort4 = __attribute__((address_space(3))) s16x4;
+
+__device__ __forceinline__ void copy16(const void *from, void *to) {
+    __builtin_amdgcn_global_load_lds((GlobalWord *)from, (LdsWord *)to, 16, 0, 0);
+}
+
+// The 16 rows that one transposing read takes (bits 0, 1, 3, 4 of d) fall on as many granules as a row of G has.
+template <int G>
+__device__ __forceinline__ int spread(int d) {
+    if constexpr (G >= 16) return (d & 3) | ((d >> 3) & 3) << 2;
+    if constexpr (G == 8) return (d & 3) | ((d >> 3) & 1) << 2;
+    return d & 3;
+}
+
+// One operand: BR rows (or columns) of the tile, copied by WAVES wavefronts, read as F fragments by each.
+template <class T, bool ACROSS, int BR, int WAVES, int F>
+struct Operand {
+    static constexpr int kBytes = BR * kDeep * 2;
+    static constexpr int kRounds = kBytes / (WAVES * 1024);
+    static_assert(kRounds * WAVES * 1024 == kBytes);
+    static constexpr int kRowBytes = ACROSS ? BR * 2 : kDeep * 2, kGranules = BR / 16;
+    const char *at[kRounds];
+    int part[ACROSS ? F : kDeep / 32];  // LDS places of the lane's parts of fragments
+
+    // Round q of the copies fills 1024 bytes a wavefront in lane order.  The lane's row (along: of the tile, across:
+    // of the step) and its first element in the row.
+    __device__ __forceinline__ static int copy_row(int q, int wave, int lane) {
+        return (q * WAVES + wave) * (1024 / kRowBytes) + lane / (kRowBytes / 16);
+    }
+    __device__ __forceinline__ static int copy_element(int q, int wave, int lane) {
+        const int r = copy_row(q, wave, lane), p = lane % (kRowBytes / 16);
+        if constexpr (!ACROSS) return (p ^ (r & 7)) * 8;
+        return ((p / 2) ^ spread<kGranules>(r)) * 16 + (p & 1) * 8;
+    }
+    // row(i): the i-th row's first element.
+    template <class Row>
+    __device__ __forceinline__ void start_along(int wave, int lane, Row row) {
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q)
+            at[q] = reinterpret_cast<const char *>(row(copy_row(q, wave, lane)) + copy_element(q, wave, lane));
+    }
+    // base: the first element of the first row's columns here, of which there are `width`.
+    __device__ __forceinline__ void start_across(int wave, int lane, const T *base, int64_t pitch, int width) {
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q)
+            at[q] = reinterpret_cast<const char *>(base + copy_row(q, wave, lane) * pitch +
+                                                   min(copy_element(q, wave, lane), width - 8));
+    }
+    // Copies a step of which `left` places of the contraction exist, and moves on by `next` bytes.
+    __device__ __forceinline__ void copy(int wave, int lane, char *lds, int left, int64_t next) {
+        if (left >= kDeep) {
+#pragma unroll
+            for (int q = 0; q < kRounds; ++q) copy16(at[q], lds + (q * WAVES + wave) * 1024);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kRounds; ++q) {
+                const int depth = ACROSS ? copy_row(q, wave, lane) : copy_element(q, wave, lane);
+                copy16(depth < left ? at[q] : reinterpret_cast<const char *>(zero_page),
+                       lds + (q * WAVES + wave) * 1024);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) at[q] += next;
+    }
+    // The wavefront's fragments begin at row `first` of the tile, a multiple of 16 F.
+    __device__ __forceinline__ void start_read(int first, int lane) {
+        if constexpr (!ACROSS) {
+#pragma unroll
+            for (int kk = 0; kk < kDeep / 32; ++kk)
+                part[kk] = (first + (lane & 15)) * 128 + ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16;
+        } else {
+            const int d = (lane >> 4) * 8 + ((lane >> 2) & 3);
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+                part[i] = d * kRowBytes + ((first / 16 + i) ^ spread<kGranules>(d)) * 32 + (lane & 3) * 8;
+        }
+    }
+    // The i-th fragment, part kk of the step.
+    __device__ __forceinline__ Frag8<T> frag(const char *lds, int i, int kk) const {
+        if constexpr (!ACROSS) {
+            return *reinterpret_cast<const Frag8<T> *>(lds + part[kk] + i * 16 * 128);
+        } else {
+            s16x4 half[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (LdsShort4 *)(lds + part[i] + (kk * 32 + h * 4) * kRowBytes));
+            const s16x8 all = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(Frag8<T>, all);
+        }
+    }
+};
+
+template <class T, int MODE, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void sk_experts_tile(ExpertArgs A) {
+    constexpr int WAVES = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
+    using OpA = Operand<T, MODE == kWeight, BM, WAVES, FM>;
+    using OpB = Operand<T, MODE != kForward, BN, WAVES, FN>;
+    __shared__ __attribute__((aligned(1024))) char a0[OpA::kBytes], b0[OpB::kBytes], a1[OpA::kBytes], b1[OpB::kBytes];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int K = A.K, N = A.N;
+    const T *x = static_cast<const T *>(A.x), *w = static_cast<const T *>(A.w), *gy = static_cast<const T *>(A.gy);
+
+    // The tile: rows [m0, m1) of the result, columns from c0, of expert e, with `deep` products to a sum.
+    int e, m0, m1, c0, deep, r0 = 0;
+    const int cols = MODE == kForward ? N : K;
+    if constexpr (MODE == kWeight) {
+        const int tn = (N + BM - 1) / BM, tk = (K + BN - 1) / BN;
+        const int t = xcd_order(blockIdx.x, A.E * tn * tk);
+        if (t < 0) return;
+        e = t / (tn * tk);
+        const int i = t - e * (tn * tk);
+        m0 = i / tk * BM, m1 = N;
+        c0 = i % tk * BN;
+        const RowRange rr = expert_rows(A, e);
+        r0 = rr.begin;
+        deep = rr.end - rr.begin;
+    } else {
+        const Tile t = find_tile(A, BM, (cols + BN - 1) / BN, blockIdx.x);
+        if (t.expert < 0) return;
+        e = t.expert, m0 = t.begin, m1 = t.end;
+        c0 = t.column * BN;
+        deep = e >= A.E ? 0 : MODE == kForward ? K : N;
+    }
+
+    f32x4 acc[FM][FN] = {};
+    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    if (deep > 0) {
+        OpA oa;
+        OpB ob;
+        oa.start_read(wm, lane);
+        ob.start_read(wn, lane);
+        int64_t next_a = kDeep * 2, next_b = kDeep * 2;
+        if constexpr (MODE == kForward) {
+            oa.start_along(wave, lane, [&](int i) {
+                const int r = min(m0 + i, m1 - 1);
+                const int t = A.tokens ? A.tokens[r] : r;
+                return x + (int64_t)(A.tokens && (t < 0 || t >= A.T) ? 0 : t) * K;
+            });
+            ob.start_along(wave, lane, [&](int i) { return w + ((int64_t)e * N + min(c0 + i, N - 1)) * K; });
+        } else if constexpr (MODE == kInput) {
+            oa.start_along(wave, lane, [&](int i) { return gy + (int64_t)min(m0 + i, m1 - 1) * N; });
+            ob.start_across(wave, lane, w + (int64_t)e * N * K + c0, K, K - c0);
+            next_b = (int64_t)kDeep * K * 2;
+        } else {
+            oa.start_across(wave, lane, gy + (int64_t)r0 * N + m0, N, N - m0);
+            next_a = (int64_t)kDeep * N * 2;
+        }
+        auto copy = [&](int d0, char *la, char *lb) {
+            oa.copy(wave, lane, la, deep - d0, next_a);
+            if constexpr (MODE != kWeight) {
+                ob.copy(wave, lane, lb, deep - d0, next_b);
+            } else {
+#pragma unroll
+                for (int q = 0; q < OpB::kRounds; ++q) {
+                    const int d = d0 + OpB::copy_row(q, wave, lane);
+                    const int col = min(c0 + OpB::copy_element(q, wave, lane), K - 8);
+                    int t = -1;
+                    if (d < deep) t = A.tokens ? A.tokens[r0 + d] : r0 + d;
+                    const bool there = t >= 0 && (!A.tokens || t < A.T);
+                    copy16(there ? reinterpret_cast<const char *>(x + (int64_t)t * K + col)
+                                 : reinterpret_cast<const char *>(zero_page),
+                           lb + (q * WAVES + wave) * 1024);
+                }
+            }
+        };
+        auto products = [&](const char *la, const char *lb) {
+#pragma unroll
+            for (int kk = 0; kk < kDeep / 32; ++kk) {
+                Frag8<T> fb[FN], fa[FM];
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = ob.frag(lb, j, kk);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[i] = oa.frag(la, i, kk);
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = mfma16<T>(fb[j], fa[i], acc[i][j]);
+            }
+        };
+        copy(0, a0, b0);
+        for (int d0 = 0; d0 < deep; d0 += 2 * kDeep) {
+            __syncthreads();  // the copies of this step have landed, and nobody reads the other buffer any more
+            if (d0 + kDeep < deep) copy(d0 + kDeep, a1, b1);
+            products(a0, b0);
+            __syncthreads();
+            if (d0 + 2 * kDeep < deep) copy(d0 + 2 * kDeep, a0, b0);
+            if (d0 + kDeep < deep) products(a1, b1);
+        }
+    }
+    // A lane holds four neighbouring columns of a row: row lane % 16, columns (lane / 16) * 4 of a 16 x 16 block.
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int row = m0 + wm + i * 16 + (lane & 15);
+        if (row >= m1) continue;
+        const int64_t base = (MODE == kWeight ? (int64_t)e * N + row : row) * (int64_t)cols;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int col = c0 + wn + j * 16 + (lane >> 4) * 4;
+            if (col >= cols) continue;
+            if (MODE == kInput && A.out32) {
+                *reinterpret_cast<f32x4 *>(A.out32 + base + col) = acc[i][j];
+            } else {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                T4 o;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) o[v] = (T)acc[i][j][v];
+                *reinterpret_cast<T4 *>(static_cast<T *>(A.out) + base + col) = o;
+            }
+        }
+    }
+}
+
 // ---- any sizes and alignment: 64 x 64 tiles, elements loaded one by one ----
 
 constexpr int kAnyTile = 64, kAnyDeep = 32, kAnyPitch = kAnyDeep + 8;
@@ -37,19 +275,20 @@ __global__ __launch_bounds__(kThreads) void sk_experts_any(ExpertArgs A) {
     int e, r0, r1, c0, m0 = 0;  // the expert, its rows here, the first column; weight: the first row of gw's tile
     if constexpr (MODE == kWeight) {
         const int tk = (K + kAnyTile - 1) / kAnyTile, tn = (N + kAnyTile - 1) / kAnyTile;
-        e = blockIdx.x / (tk * tn);
-        const int rest = blockIdx.x - e * (tk * tn);
+        const int t = xcd_order(blockIdx.x, A.E * tk * tn);
+        if (t < 0) return;
+        e = t / (tk * tn);
+        const int rest = t - e * (tk * tn);
         m0 = rest / tk * kAnyTile;
         c0 = rest % tk * kAnyTile;
         const RowRange rr = expert_rows(A, e);
         r0 = rr.begin, r1 = rr.end;
     } else {
         const int cols = MODE == kForward ? N : K;
-        const int tc = (cols + kAnyTile - 1) / kAnyTile;
-        const RowTile t = find_row_tile(A, kAnyTile, blockIdx.x / tc);
+        const Tile t = find_tile(A, kAnyTile, (cols + kAnyTile - 1) / kAnyTile, blockIdx.x);
         if (t.expert < 0) return;
         e = t.expert, r0 = t.begin, r1 = t.end;
-        c0 = blockIdx.x % tc * kAnyTile;
+        c0 = t.column * kAnyTile;
     }
     const T *we = w + (size_t)(e < A.E ? e : 0) * N * K;
     const int deep = MODE == kForward ? K : MODE == kInput ? N : r1 - r0;
@@ -167,14 +406,39 @@ int64_t most_row_tiles(const ExpertArgs &a, int tile) {
     const int64_t rows = (int64_t)a.T * a.k;
     return rows / tile + (rows < a.E + 1 ? rows : a.E + 1);
 }
+int64_t parts(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-template <int MODE>
-hipError_t launch_rows(const ExpertArgs &a, hipStream_t st) {
-    const int cols = MODE == kForward ? a.N : a.K;
-    const int64_t grid = most_row_tiles(a, kAnyTile) * ((cols + kAnyTile - 1) / kAnyTile);
+template <int MODE, int BM, int BN, int WM, int WN>
+hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
+    const int64_t tiles = MODE == kWeight ? a.E * parts(a.N, BM) * parts(a.K, BN)
+                                          : most_row_tiles(a, BM) * parts(MODE == kForward ? a.N : a.K, BN);
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
-        hipLaunchKernelGGL((sk_experts_any<T, MODE>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL((sk_experts_tile<T, MODE, BM, BN, WM, WN>), dim3((unsigned)(parts(tiles, 8) * 8)),
+                           dim3(WM * WN * 64), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+// Whether rows can be copied in chunks of 16 bytes.
+bool chunks(const ExpertArgs &a) {
+    return a.K % 8 == 0 && a.N % 8 == 0 && (!a.x || aligned16(a.x)) && (!a.w || aligned16(a.w)) &&
+           (!a.gy || aligned16(a.gy)) && aligned16(a.out) && aligned16(a.out32);
+}
+
+template <int MODE>
+hipError_t launch_product(const ExpertArgs &a, hipStream_t st) {
+    if (chunks(a)) {
+        const int64_t rows = (int64_t)a.T * a.k;
+        const int64_t m = MODE == kWeight ? a.N : rows / a.E, c = MODE == kForward ? a.N : a.K;
+        if (m > 128 && c > 128) return launch_tile<MODE, 256, 256, 2, 4>(a, st);
+        return launch_tile<MODE, 128, 128, 2, 2>(a, st);
+    }
+    const int64_t cols = parts(MODE == kForward ? a.N : a.K, kAnyTile);
+    const int64_t grid = cols * (MODE == kWeight ? a.E * parts(a.N, kAnyTile) : most_row_tiles(a, kAnyTile));
+    return with_half(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        hipLaunchKernelGGL((sk_experts_any<T, MODE>), dim3((unsigned)(parts(grid, 8) * 8)), dim3(kThreads), 0, st, a);
         return hipGetLastError();
     });
 }
@@ -185,15 +449,15 @@ size_t experts_workspace_bytes(int T, int k, int K) { return (size_t)T * k * K *
 
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    return launch_rows<kForward>(a, st);
+    return launch_product<kForward>(a, st);
 }
 
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    if (!a.slots) return launch_rows<kInput>(a, st);
+    if (!a.slots) return launch_product<kInput>(a, st);
     ExpertArgs r = a;
     r.out32 = static_cast<float *>(ws);
-    const hipError_t e = launch_rows<kInput>(r, st);
+    const hipError_t e = launch_product<kInput>(r, st);
     if (e != hipSuccess) return e;
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
@@ -209,12 +473,7 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
 }
 
 hipError_t launch_experts_weight(const ExpertArgs &a, hipStream_t st) {
-    const int64_t grid = (int64_t)a.E * ((a.N + kAnyTile - 1) / kAnyTile) * ((a.K + kAnyTile - 1) / kAnyTile);
-    return with_half(a.dtype, [&](auto type) {
-        using T = decltype(type);
-        hipLaunchKernelGGL((sk_experts_any<T, kWeight>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
-        return hipGetLastError();
-    });
+    return launch_product<kWeight>(a, st);
 }
 
 }  // namespace sk
