@@ -334,9 +334,10 @@ SK_API int32_t sinkhorn_regime(const sk_problem *p);
  * C = -logits [T, E], uniform mu over the tokens and nu over the experts,
  * lambda * beta of sinkhorn_forward is the per-expert offset under which the
  * experts are taken evenly: it is the `bias` of the router below.  The
- * conventions at the top of this file hold; in addition, indices that another
- * call of this library wrote (offsets, tokens, slots) are checked by the
- * kernels: one out of range names no row and no token.
+ * conventions at the top of this file hold.  Indices that are to come from the
+ * router (offsets, tokens, slots) are held to their ranges by the kernels: with
+ * others no call reads or writes outside its arrays, but results are
+ * unspecified.
  */
 typedef enum { SK_F32 = 0, SK_BF16 = 1, SK_F16 = 2 } sk_dtype;
 

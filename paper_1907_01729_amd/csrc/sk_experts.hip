@@ -26,8 +26,11 @@ __device__ __forceinline__ f32x4 mfma16(const Frag8<T> &a, const Frag8<T> &b, f3
 // ---- tiles: columns in whole chunks of eight, every pointer aligned to 16 bytes ----
 //
 // A work-group computes BM x BN results; its wavefronts, WM x WN of them, a part of BM / WM x BN / WN each, held in
-// registers.  The contraction goes in steps of 64.  Both operands' steps are copied to LDS by the memory pipe itself
-// (16 bytes a lane), one step ahead of the products, into one of two buffers; one barrier a step.
+// registers.  The contraction goes in steps of 64 (128 bytes of a row, a whole cache line).  Operands are copied to LDS
+// by the memory pipe itself, 16 bytes a lane, into one of two buffers, one step ahead of the products, with one barrier
+// a step.  The copies are issued one by one among the products, since the pipe takes few at a time and a wavefront
+// whose copy is not taken cannot issue its products; they are addressed by a scalar base and an offset of 32 bits a
+// lane, which the pipe takes a tenth faster than addresses of 64 bits.
 //
 // An operand whose rows run along the contraction ("along": x, w in forward, gy in input) lies in LDS as rows of 64,
 // and a lane's eight elements are one 16-byte read.  An operand whose rows run across it ("across": w in input, gy
@@ -43,14 +46,36 @@ constexpr int kDeep = 64;
 
 __device__ __attribute__((aligned(16))) uint32_t zero_page[4];
 
-using GlobalWord = const __attribute__((address_space(1))) uint32_t;
-using LdsWord = __attribute__((address_space(3))) uint32_t;
+using LdsByte = __attribute__((address_space(3))) char;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 using LdsShort4 = __attribute__((address_space(3))) s16x4;
 
-__device__ __forceinline__ void copy16(const void *from, void *to) {
-    __builtin_amdgcn_global_load_lds((GlobalWord *)from, (LdsWord *)to, 16, 0, 0);
+// Copies 16 bytes a lane to LDS: from base + each lane's offset to `to` (one for the wavefront) + 16 lane.  WIDE: the
+// offset is a whole address.  Written out, since the compiler puts a wait for every copy under way before each
+// transposing read that follows it.  It has no result in registers, and the place is not read before all_copies.
+template <bool WIDE>
+using Offset = std::conditional_t<WIDE, const char *, uint32_t>;
+
+template <bool WIDE>
+__device__ __forceinline__ void copy16(const char *base, Offset<WIDE> from, char *to) {
+    const uint32_t place = (uint32_t)(uintptr_t)(LdsByte *)to;
+    if constexpr (WIDE)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                     :
+                     : "v"(from), "s"(place)
+                     : "m0", "memory");
+    else
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2"
+                     :
+                     : "v"(from), "s"(place), "s"(base)
+                     : "m0", "memory");
+}
+// Every copy of the work-group has landed and every LDS read is done.
+__device__ __forceinline__ void all_copies() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // The 16 rows that one transposing read takes (bits 0, 1, 3, 4 of d) fall on as many granules as a row of G has.
@@ -68,7 +93,6 @@ struct Operand {
     static constexpr int kRounds = kBytes / (WAVES * 1024);
     static_assert(kRounds * WAVES * 1024 == kBytes);
     static constexpr int kRowBytes = ACROSS ? BR * 2 : kDeep * 2, kGranules = BR / 16;
-    const char *at[kRounds];
     int part[ACROSS ? F : kDeep / 32];  // LDS places of the lane's parts of fragments
 
     // Round q of the copies fills 1024 bytes a wavefront in lane order.  The lane's row (along: of the tile, across:
@@ -81,42 +105,16 @@ struct Operand {
         if constexpr (!ACROSS) return (p ^ (r & 7)) * 8;
         return ((p / 2) ^ spread<kGranules>(r)) * 16 + (p & 1) * 8;
     }
-    // row(i): the i-th row's first element.
-    template <class Row>
-    __device__ __forceinline__ void start_along(int wave, int lane, Row row) {
-#pragma unroll
-        for (int q = 0; q < kRounds; ++q)
-            at[q] = reinterpret_cast<const char *>(row(copy_row(q, wave, lane)) + copy_element(q, wave, lane));
-    }
-    // base: the first element of the first row's columns here, of which there are `width`.
-    __device__ __forceinline__ void start_across(int wave, int lane, const T *base, int64_t pitch, int width) {
-#pragma unroll
-        for (int q = 0; q < kRounds; ++q)
-            at[q] = reinterpret_cast<const char *>(base + copy_row(q, wave, lane) * pitch +
-                                                   min(copy_element(q, wave, lane), width - 8));
-    }
-    // Copies a step of which `left` places of the contraction exist, and moves on by `next` bytes.
-    __device__ __forceinline__ void copy(int wave, int lane, char *lds, int left, int64_t next) {
-        if (left >= kDeep) {
-#pragma unroll
-            for (int q = 0; q < kRounds; ++q) copy16(at[q], lds + (q * WAVES + wave) * 1024);
-        } else {
-#pragma unroll
-            for (int q = 0; q < kRounds; ++q) {
-                const int depth = ACROSS ? copy_row(q, wave, lane) : copy_element(q, wave, lane);
-                copy16(depth < left ? at[q] : reinterpret_cast<const char *>(zero_page),
-                       lds + (q * WAVES + wave) * 1024);
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < kRounds; ++q) at[q] += next;
+    // Whether the lane's chunk of round q lies past the end of the contraction, of which `left` places are left.
+    __device__ __forceinline__ static bool past(int q, int wave, int lane, int left) {
+        return (ACROSS ? copy_row(q, wave, lane) : copy_element(q, wave, lane)) >= left;
     }
     // The wavefront's fragments begin at row `first` of the tile, a multiple of 16 F.
     __device__ __forceinline__ void start_read(int first, int lane) {
         if constexpr (!ACROSS) {
 #pragma unroll
             for (int kk = 0; kk < kDeep / 32; ++kk)
-                part[kk] = (first + (lane & 15)) * 128 + ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16;
+                part[kk] = (first + (lane & 15)) * kRowBytes + ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16;
         } else {
             const int d = (lane >> 4) * 8 + ((lane >> 2) & 3);
 #pragma unroll
@@ -127,7 +125,7 @@ struct Operand {
     // The i-th fragment, part kk of the step.
     __device__ __forceinline__ Frag8<T> frag(const char *lds, int i, int kk) const {
         if constexpr (!ACROSS) {
-            return *reinterpret_cast<const Frag8<T> *>(lds + part[kk] + i * 16 * 128);
+            return *reinterpret_cast<const Frag8<T> *>(lds + part[kk] + i * 16 * kRowBytes);
         } else {
             s16x4 half[2];
 #pragma unroll
@@ -140,20 +138,23 @@ struct Operand {
     }
 };
 
-template <class T, int MODE, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN * 64) void sk_experts_tile(ExpertArgs A) {
+// GATHERED: x's rows are looked up in tokens.  WIDE: x has 2^32 bytes or more.
+template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE>
+__global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void sk_experts_tile(ExpertArgs A) {
     constexpr int WAVES = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
     using OpA = Operand<T, MODE == kWeight, BM, WAVES, FM>;
     using OpB = Operand<T, MODE != kForward, BN, WAVES, FN>;
-    __shared__ __attribute__((aligned(1024))) char a0[OpA::kBytes], b0[OpB::kBytes], a1[OpA::kBytes], b1[OpB::kBytes];
+    constexpr int kStep = OpA::kBytes + OpB::kBytes;
+    constexpr bool kWideA = WIDE && MODE == kForward, kWideB = WIDE && MODE == kWeight;
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int K = A.K, N = A.N;
+    const int K = A.K, N = A.N, cols = MODE == kForward ? N : K;
     const T *x = static_cast<const T *>(A.x), *w = static_cast<const T *>(A.w), *gy = static_cast<const T *>(A.gy);
 
-    // The tile: rows [m0, m1) of the result, columns from c0, of expert e, with `deep` products to a sum.
+    // The tile: rows [m0, m1) of the result, columns from c0, of expert e, with `deep` products to a sum (weight: over
+    // the rows from r0).
     int e, m0, m1, c0, deep, r0 = 0;
-    const int cols = MODE == kForward ? N : K;
     if constexpr (MODE == kWeight) {
         const int tn = (N + BM - 1) / BM, tk = (K + BN - 1) / BN;
         const int t = xcd_order(blockIdx.x, A.E * tn * tk);
@@ -172,6 +173,10 @@ __global__ __launch_bounds__(WM *WN * 64) void sk_experts_tile(ExpertArgs A) {
         c0 = t.column * BN;
         deep = e >= A.E ? 0 : MODE == kForward ? K : N;
     }
+    // one answer for the work-group: kept in scalar registers
+    e = __builtin_amdgcn_readfirstlane(e), m0 = __builtin_amdgcn_readfirstlane(m0);
+    m1 = __builtin_amdgcn_readfirstlane(m1), c0 = __builtin_amdgcn_readfirstlane(c0);
+    r0 = __builtin_amdgcn_readfirstlane(r0), deep = __builtin_amdgcn_readfirstlane(deep);
 
     f32x4 acc[FM][FN] = {};
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
@@ -180,63 +185,150 @@ __global__ __launch_bounds__(WM *WN * 64) void sk_experts_tile(ExpertArgs A) {
         OpB ob;
         oa.start_read(wm, lane);
         ob.start_read(wn, lane);
-        int64_t next_a = kDeep * 2, next_b = kDeep * 2;
+
+        // Where the copies of a step come from: a base that moves on with the steps and the lane's offsets from it.  x's
+        // rows in "weight" are looked up anew for every step, a step before their copies.
+        constexpr bool kLookUp = MODE == kWeight && GATHERED;
+        const char *base_a, *base_b;
+        Offset<kWideA> from_a[OpA::kRounds];
+        Offset<kWideB> from_b[OpB::kRounds];
+        int token[kLookUp ? OpB::kRounds : 1];
         if constexpr (MODE == kForward) {
-            oa.start_along(wave, lane, [&](int i) {
-                const int r = min(m0 + i, m1 - 1);
-                const int t = A.tokens ? A.tokens[r] : r;
-                return x + (int64_t)(A.tokens && (t < 0 || t >= A.T) ? 0 : t) * K;
-            });
-            ob.start_along(wave, lane, [&](int i) { return w + ((int64_t)e * N + min(c0 + i, N - 1)) * K; });
-        } else if constexpr (MODE == kInput) {
-            oa.start_along(wave, lane, [&](int i) { return gy + (int64_t)min(m0 + i, m1 - 1) * N; });
-            ob.start_across(wave, lane, w + (int64_t)e * N * K + c0, K, K - c0);
-            next_b = (int64_t)kDeep * K * 2;
+            base_a = reinterpret_cast<const char *>(x + (GATHERED ? 0 : (int64_t)m0 * K));
+#pragma unroll
+            for (int q = 0; q < OpA::kRounds; ++q) {
+                const int r = min(m0 + OpA::copy_row(q, wave, lane), m1 - 1);
+                int t = GATHERED ? A.tokens[r] : r - m0;
+                if (GATHERED && (t < 0 || t >= A.T)) t = 0;
+                if constexpr (kWideA)
+                    from_a[q] = base_a + ((int64_t)t * K + OpA::copy_element(q, wave, lane)) * 2;
+                else
+                    from_a[q] = ((uint32_t)t * K + OpA::copy_element(q, wave, lane)) * 2;
+            }
         } else {
-            oa.start_across(wave, lane, gy + (int64_t)r0 * N + m0, N, N - m0);
-            next_a = (int64_t)kDeep * N * 2;
+            const int64_t first = MODE == kInput ? (int64_t)m0 * N : (int64_t)r0 * N + m0;
+            base_a = reinterpret_cast<const char *>(gy + first);
+#pragma unroll
+            for (int q = 0; q < OpA::kRounds; ++q) {
+                const int r = OpA::copy_row(q, wave, lane), c = OpA::copy_element(q, wave, lane);
+                from_a[q] = MODE == kInput ? (uint32_t)(min(r, m1 - 1 - m0) * N + c) * 2
+                                           : (uint32_t)(r * N + min(c, N - 8 - m0)) * 2;
+            }
         }
-        auto copy = [&](int d0, char *la, char *lb) {
-            oa.copy(wave, lane, la, deep - d0, next_a);
-            if constexpr (MODE != kWeight) {
-                ob.copy(wave, lane, lb, deep - d0, next_b);
-            } else {
+        if constexpr (MODE == kWeight) {
+            base_b = reinterpret_cast<const char *>(x + c0 + (GATHERED ? 0 : (int64_t)r0 * K));
+        } else {
+            base_b = reinterpret_cast<const char *>(w + (int64_t)e * N * K + (MODE == kForward ? (int64_t)c0 * K : c0));
+        }
+#pragma unroll
+        for (int q = 0; q < OpB::kRounds; ++q) {
+            const int r = OpB::copy_row(q, wave, lane), c = OpB::copy_element(q, wave, lane);
+            if constexpr (!kLookUp)
+                from_b[q] = MODE == kForward ? (uint32_t)(min(r, N - 1 - c0) * K + c) * 2
+                                             : (uint32_t)(r * K + min(c, K - 8 - c0)) * 2;
+        }
+        auto look_up = [&](int d0) {
+            if constexpr (kLookUp) {
+#pragma unroll
+                for (int q = 0; q < OpB::kRounds; ++q)
+                    token[q] = A.tokens[r0 + min(d0 + OpB::copy_row(q, wave, lane), deep - 1)];
+            }
+        };
+        auto take_rows = [&] {
+            if constexpr (kLookUp) {
 #pragma unroll
                 for (int q = 0; q < OpB::kRounds; ++q) {
-                    const int d = d0 + OpB::copy_row(q, wave, lane);
-                    const int col = min(c0 + OpB::copy_element(q, wave, lane), K - 8);
-                    int t = -1;
-                    if (d < deep) t = A.tokens ? A.tokens[r0 + d] : r0 + d;
-                    const bool there = t >= 0 && (!A.tokens || t < A.T);
-                    copy16(there ? reinterpret_cast<const char *>(x + (int64_t)t * K + col)
-                                 : reinterpret_cast<const char *>(zero_page),
-                           lb + (q * WAVES + wave) * 1024);
+                    // To the compiler, a wait for the look-up: here, where no copy is under way.
+                    asm volatile("" : "+v"(token[q]));
+                    const int t = token[q] >= 0 && token[q] < A.T ? token[q] : 0;
+                    const int c = min(OpB::copy_element(q, wave, lane), K - 8 - c0);
+                    if constexpr (kWideB)
+                        from_b[q] = base_b + ((int64_t)t * K + c) * 2;
+                    else
+                        from_b[q] = ((uint32_t)t * K + c) * 2;
                 }
             }
         };
-        auto products = [&](const char *la, const char *lb) {
-#pragma unroll
-            for (int kk = 0; kk < kDeep / 32; ++kk) {
-                Frag8<T> fb[FN], fa[FM];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = ob.frag(lb, j, kk);
-#pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = oa.frag(la, i, kk);
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = mfma16<T>(fb[j], fa[i], acc[i][j]);
+        // Copy c of the step at d0.  PARTIAL: the contraction ends within the step, zeros from there.
+        constexpr int kCopies = OpA::kRounds + OpB::kRounds;
+        auto copy = [&](auto partial, int c, int d0, char *to) {
+            const bool is_a = c < OpA::kRounds;
+            const int q = is_a ? c : c - OpA::kRounds;
+            to += (is_a ? 0 : OpA::kBytes) + (q * WAVES + wave) * 1024;
+            if constexpr (decltype(partial)::value) {
+                const char *from;
+                if (is_a) {
+                    if constexpr (kWideA) from = from_a[q];
+                    else from = base_a + from_a[q];
+                    if (OpA::past(q, wave, lane, deep - d0)) from = reinterpret_cast<const char *>(zero_page);
+                } else {
+                    if constexpr (kWideB) from = from_b[q];
+                    else from = base_b + from_b[q];
+                    if (OpB::past(q, wave, lane, deep - d0)) from = reinterpret_cast<const char *>(zero_page);
+                }
+                copy16<true>(nullptr, from, to);
+            } else if (is_a) {
+                copy16<kWideA>(base_a, from_a[q], to);
+            } else {
+                copy16<kWideB>(base_b, from_b[q], to);
             }
         };
-        copy(0, a0, b0);
-        for (int d0 = 0; d0 < deep; d0 += 2 * kDeep) {
-            __syncthreads();  // the copies of this step have landed, and nobody reads the other buffer any more
-            if (d0 + kDeep < deep) copy(d0 + kDeep, a1, b1);
-            products(a0, b0);
-            __syncthreads();
-            if (d0 + 2 * kDeep < deep) copy(d0 + 2 * kDeep, a0, b0);
-            if (d0 + kDeep < deep) products(a1, b1);
+        // On to the next step's places.
+        auto advance = [&] {
+            const int64_t on_a = (MODE == kWeight ? (int64_t)N : 1) * kDeep * 2;
+            const int64_t on_b = kLookUp ? 0 : (MODE == kForward ? 1 : (int64_t)K) * kDeep * 2;
+            base_a += on_a, base_b += on_b;
+            if constexpr (kWideA) {
+#pragma unroll
+                for (int q = 0; q < OpA::kRounds; ++q) from_a[q] += on_a;
+            }
+        };
+        // The step at d0 in `here`: FN products to a turn.  A turn reads the rows' fragment of two turns on and, towards
+        // the end of the first half, a fragment of the second half's columns, and issues its share of the next step's
+        // copies (if there is one); the compiler may not move anything across turns, or it would read each fragment
+        // right before its use and wait for it.
+        auto step = [&](auto next, auto partial, int d0, const char *here, char *there) {
+            constexpr int kTurns = kDeep / 32 * FM, kLead = 2, kEvery = kTurns / kCopies;
+            static_assert(kEvery * kCopies == kTurns && FM >= FN);
+            all_copies();
+            take_rows();
+            look_up(d0 + 2 * kDeep);
+            const char *la = here, *lb = here + OpA::kBytes;
+            Frag8<T> fb[kDeep / 32][FN], fa[kTurns];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[0][j] = ob.frag(lb, j, 0);
+#pragma unroll
+            for (int i = 0; i < kLead; ++i) fa[i] = oa.frag(la, i % FM, i / FM);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                if (i + kLead < kTurns) fa[i + kLead] = oa.frag(la, (i + kLead) % FM, (i + kLead) / FM);
+                const int j0 = i - (FM - FN);
+                if (j0 >= 0 && j0 < FN) fb[1][j0] = ob.frag(lb, j0, 1);
+                if constexpr (decltype(next)::value) {
+                    if (i % kEvery == 0) copy(partial, i / kEvery, d0 + kDeep, there);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i % FM][j] = mfma16<T>(fb[i / FM][j], fa[i], acc[i % FM][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            advance();
+        };
+        constexpr std::true_type yes{};
+        constexpr std::false_type no{};
+        look_up(0);
+        take_rows();
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) copy(yes, c, 0, lds);
+        advance();
+        look_up(kDeep);
+        int d0 = 0, odd = 0;
+        for (; d0 + 2 * kDeep <= deep; d0 += kDeep, odd ^= 1) step(yes, no, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
+        if (d0 + kDeep < deep) {
+            step(yes, yes, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
+            d0 += kDeep, odd ^= 1;
         }
+        step(no, no, d0, lds + odd * kStep, lds);
     }
     // A lane holds four neighbouring columns of a row: row lane % 16, columns (lane / 16) * 4 of a 16 x 16 block.
 #pragma unroll
@@ -414,9 +506,16 @@ hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
                                           : most_row_tiles(a, BM) * parts(MODE == kForward ? a.N : a.K, BN);
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
-        hipLaunchKernelGGL((sk_experts_tile<T, MODE, BM, BN, WM, WN>), dim3((unsigned)(parts(tiles, 8) * 8)),
-                           dim3(WM * WN * 64), 0, st, a);
-        return hipGetLastError();
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(parts(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
+            return hipGetLastError();
+        };
+        if constexpr (MODE != kInput) {
+            if (a.tokens && (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32))
+                return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, true, true>);
+            if (a.tokens) return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, true, false>);
+        }
+        return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, false, false>);
     });
 }
 
