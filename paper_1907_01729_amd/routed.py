@@ -13,13 +13,15 @@ tokens spread evenly over the experts; it goes into ``sinkhorn_route`` as ``bias
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple
 
 import torch
 
-from ._binding import (SinkhornError, SkCombine, SkExperts, SkRouter, _dev, _on, _ptr, _stream, load_library)
+from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, load_library
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_HALF = {torch.bfloat16: 1, torch.float16: 2}
 _U64 = (1 << 64) - 1
 
 
@@ -35,7 +37,9 @@ class Routing(NamedTuple):
     z_loss: torch.Tensor   # [] float32, differentiable
 
 
-def _typed(t, name, allowed=tuple(_DTYPE)):
+# ---- checks and calls ----
+
+def _typed(t, name, allowed=_DTYPE):
     """A contiguous GPU tensor of one of the element types the operators take."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
@@ -46,85 +50,140 @@ def _typed(t, name, allowed=tuple(_DTYPE)):
     return t
 
 
-def _shape(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
+def _match(t, name, ref, shape=None, dtype=None):
+    """A contiguous GPU tensor on ref's device, of the dtype and shape given."""
+    if dtype is not None:
+        _dev(t, name, dtype)
+    if t.device != ref.device:
+        raise ValueError(f"{name} must be on {ref.device}, got {t.device}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
-def _like(t, ref, name):
-    if t.device != ref.device:
-        raise ValueError(f"{name} must be on {ref.device}, got {t.device}")
+# The current stream's handle.  The public property builds a Stream object for it, which takes twenty times as long.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-
-def _call(fn, dev, stream, *args):
-    """fn(*args, stream) on dev, whichever device is current."""
-    if torch.cuda.current_device() == dev.index:
-        st = fn(*args, _stream(dev, stream))
+def _call(fn, dev, *args):
+    """fn(*args, stream): on dev's current stream, whichever device is current."""
+    index = dev.index
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(dev):
-            st = fn(*args, _stream(dev, stream))
-    if st != 0:
-        raise SinkhornError(st, fn.__name__)
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != 0:
+        raise SinkhornError(status, fn.__name__)
+
+
+def _on_stream(fn):
+    """Gives fn a keyword argument stream: the call, its outputs and its workspace on that stream."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kwargs):
+        if stream is None:
+            return fn(*args, **kwargs)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kwargs)
+    return call
+
+
+# A call's sizes as the library takes them, and the bytes of workspace they need: functions of the sizes alone.
+@functools.lru_cache(maxsize=1024)
+def _router(T, E, k, dtype, renormalize):
+    r = SkRouter(T, E, k, dtype, renormalize)
+    return ctypes.byref(r), int(load_library().sinkhorn_route_workspace_bytes(ctypes.byref(r)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _experts(T, k, E, K, N, dtype):
+    p = SkExperts(T, k, E, K, N, dtype)
+    return ctypes.byref(p), int(load_library().sinkhorn_experts_workspace_bytes(ctypes.byref(p)))
+
+
+@functools.lru_cache(maxsize=1024)
+def _combine(T, D, k, dtype):
+    return ctypes.byref(SkCombine(T, D, k, dtype))
+
+
+def _scratch(workspace, need, dev):
+    if not need:
+        return None
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty((need,), device=dev, dtype=torch.uint8)
+    return workspace
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _counter(p, seed, offset):
     if not 0.0 <= p < 1.0:
         raise ValueError(f"p must be in [0, 1), got {p}")
-    return ctypes.c_double(p), ctypes.c_uint64(int(seed) & _U64), ctypes.c_uint64(int(offset) & _U64)
+    return float(p), int(seed) & _U64, int(offset) & _U64
 
 
 # ---- router ----
 
-def sinkhorn_route_forward(logits, k, bias=None, mask=None, renormalize=True, stream=None, workspace=None):
+@_on_stream
+def sinkhorn_route_forward(logits, k, bias=None, mask=None, renormalize=True, workspace=None):
     """logits [T, E] float32, bfloat16 or float16; bias [E] float32; mask [T] bool (False: no token).
-    Returns (Routing, state); state goes to sinkhorn_route_backward."""
-    lib = load_library()
+    Returns (Routing, state); state goes to sinkhorn_route_backward.  stream=: as in sinkhorn_forward."""
     _typed(logits, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must be [T, E], got {list(logits.shape)}")
     T, E = logits.shape
+    k = int(k)
     if bias is not None:
-        _dev(bias, "bias"), _shape(bias, (E,), "bias"), _like(bias, logits, "bias")
+        _match(bias, "bias", logits, (E,), torch.float32)
     if mask is not None:
-        _dev(mask, "mask", torch.bool), _shape(mask, (T,), "mask"), _like(mask, logits, "mask")
-    r = SkRouter(T, E, int(k), _DTYPE[logits.dtype], int(bool(renormalize)))
-    dev = logits.device
-    need = int(lib.sinkhorn_route_workspace_bytes(ctypes.byref(r)))
-    with _on(stream):
-        n = T * max(int(k), 0)
-        whole = torch.empty((3 * n + 2 * E + 1,), device=dev, dtype=torch.int32)
-        real = torch.empty((n + 2 * T + 3,), device=dev, dtype=torch.float32)
-        if need and (workspace is None or workspace.numel() < need):
-            workspace = torch.empty((need,), device=dev, dtype=torch.uint8)
-    experts, slots, tokens, counts, offsets = whole.split((n, n, n, E, E + 1))
-    weights, state, balance, z = real.split((n, 2 * T + 1, 1, 1))
-    _call(lib.sinkhorn_route_forward, dev, stream, ctypes.byref(r), _ptr(logits), _ptr(bias), _ptr(mask),
-          _ptr(weights), _ptr(experts), _ptr(counts), _ptr(offsets), _ptr(tokens), _ptr(slots), _ptr(balance),
-          _ptr(z), _ptr(state), _ptr(workspace) if need else None, ctypes.c_size_t(need))
-    return Routing(weights.view(T, k), experts.view(T, k), counts, offsets, tokens, slots.view(T, k),
-                   balance.view(()), z.view(())), state
+        _match(mask, "mask", logits, (T,), torch.bool)
+    r, need = _router(T, E, k, _DTYPE[logits.dtype], int(bool(renormalize)))
+    dev, n = logits.device, max(k, 0)
+    whole, real = {"device": dev, "dtype": torch.int32}, {"device": dev, "dtype": torch.float32}
+    weights, experts, slots = torch.empty((T, n), **real), torch.empty((T, n), **whole), torch.empty((T, n), **whole)
+    tokens, counts, offsets = (torch.empty((T * n,), **whole), torch.empty((E,), **whole),
+                               torch.empty((E + 1,), **whole))
+    balance, z, state = torch.empty((), **real), torch.empty((), **real), torch.empty((2 * T + 1,), **real)
+    scratch = _scratch(workspace, need, dev)
+    _call(load_library().sinkhorn_route_forward, dev, r, logits.data_ptr(), _ptr(bias), _ptr(mask),
+          weights.data_ptr(), experts.data_ptr(), counts.data_ptr(), offsets.data_ptr(), tokens.data_ptr(),
+          slots.data_ptr(), balance.data_ptr(), z.data_ptr(), state.data_ptr(), _ptr(scratch), need)
+    return Routing(weights, experts, counts, offsets, tokens, slots, balance, z), state
 
 
+@_on_stream
 def sinkhorn_route_backward(logits, k, weights, experts, counts, state, grad_weights=None, grad_balance=None,
-                            grad_z=None, renormalize=True, stream=None):
+                            grad_z=None, renormalize=True):
     """Gradient of the logits from those of weights, balance and z_loss (each may be None)."""
-    lib = load_library()
     _typed(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [T, E], got {list(logits.shape)}")
     T, E = logits.shape
     for t, n, shape, typ in ((weights, "weights", (T, k), torch.float32), (experts, "experts", (T, k), torch.int32),
-                             (counts, "counts", (E,), torch.int32), (state, "state", (2 * T + 1,), torch.float32),
-                             (grad_weights, "grad_weights", (T, k), torch.float32),
-                             (grad_balance, "grad_balance", (), torch.float32),
-                             (grad_z, "grad_z", (), torch.float32)):
-        if t is not None or n in ("weights", "experts", "counts", "state"):
-            _dev(t, n, typ), _shape(t, shape, n), _like(t, logits, n)
-    r = SkRouter(T, E, int(k), _DTYPE[logits.dtype], int(bool(renormalize)))
-    with _on(stream):
-        grad = torch.empty_like(logits)
-    _call(lib.sinkhorn_route_backward, logits.device, stream, ctypes.byref(r), _ptr(logits), _ptr(weights),
-          _ptr(experts), _ptr(counts), _ptr(state), _ptr(grad_weights), _ptr(grad_balance), _ptr(grad_z), _ptr(grad))
+                             (counts, "counts", (E,), torch.int32), (state, "state", (2 * T + 1,), torch.float32)):
+        _match(t, n, logits, shape, typ)
+    for t, n, shape in ((grad_weights, "grad_weights", (T, k)), (grad_balance, "grad_balance", ()),
+                        (grad_z, "grad_z", ())):
+        if t is not None:
+            _match(t, n, logits, shape, torch.float32)
+    return _route_backward(logits, int(k), weights, experts, counts, state, grad_weights, grad_balance, grad_z,
+                           renormalize)
+
+
+def _route_backward(logits, k, weights, experts, counts, state, grad_weights, grad_balance, grad_z, renormalize):
+    T, E = logits.shape
+    r, _ = _router(T, E, k, _DTYPE[logits.dtype], int(bool(renormalize)))
+    grad = torch.empty_like(logits)
+    _call(load_library().sinkhorn_route_backward, logits.device, r, logits.data_ptr(), weights.data_ptr(),
+          experts.data_ptr(), counts.data_ptr(), state.data_ptr(), _ptr(grad_weights), _ptr(grad_balance),
+          _ptr(grad_z), grad.data_ptr())
     return grad
+
+
+def _contiguous(g):
+    return None if g is None else g.contiguous()
 
 
 class _Route(torch.autograd.Function):
@@ -132,17 +191,16 @@ class _Route(torch.autograd.Function):
     def forward(ctx, logits, k, bias, mask, renormalize):
         r, state = sinkhorn_route_forward(logits, k, bias, mask, renormalize)
         ctx.save_for_backward(logits, r.weights, r.experts, r.counts, state)
-        ctx.k, ctx.renormalize = k, renormalize
+        ctx.k, ctx.renormalize = int(k), renormalize
         ctx.mark_non_differentiable(r.experts, r.counts, r.offsets, r.tokens, r.slots)
-        ctx.set_materialize_grads(False)
+        ctx.set_materialize_grads(False)  # no zeros for outputs without a gradient
         return tuple(r)
 
     @staticmethod
     def backward(ctx, g_weights, _e, _c, _o, _t, _s, g_balance, g_z):
         logits, weights, experts, counts, state = ctx.saved_tensors
-        c = lambda g: None if g is None else g.contiguous()  # noqa: E731
-        return sinkhorn_route_backward(logits, ctx.k, weights, experts, counts, state, c(g_weights), c(g_balance),
-                                       c(g_z), ctx.renormalize), None, None, None, None
+        return _route_backward(logits, ctx.k, weights, experts, counts, state, _contiguous(g_weights),
+                               _contiguous(g_balance), _contiguous(g_z), ctx.renormalize), None, None, None, None
 
 
 def sinkhorn_route(logits, k, bias=None, mask=None, renormalize=True) -> Routing:
@@ -152,101 +210,101 @@ def sinkhorn_route(logits, k, bias=None, mask=None, renormalize=True) -> Routing
     logits = logits.contiguous()
     bias = None if bias is None else bias.detach().contiguous()
     mask = None if mask is None else mask.contiguous()
-    if torch.is_grad_enabled() and logits.requires_grad:
+    if logits.requires_grad and torch.is_grad_enabled():
         return Routing(*_Route.apply(logits, k, bias, mask, renormalize))
     return sinkhorn_route_forward(logits, k, bias, mask, renormalize)[0]
 
 
 # ---- experts' products ----
 
-_HALF = (torch.bfloat16, torch.float16)
-
-
-def _experts(rows, x_shape, w_shape, offsets, index, dtype, name):
-    """The SkExperts of a call: rows = T k; index: slots [T, k], tokens [T k] or None."""
-    E, N, K = w_shape
-    T, k = (rows, 1) if x_shape is None else (x_shape[0], rows // max(x_shape[0], 1))
-    if T * k != rows or (rows and k < 1):
+def _rows_of(rows, T, name):
+    """Pairs of a token, where `rows` rows belong to T tokens."""
+    if T == 0:
+        if rows:
+            raise ValueError(f"{name}: {rows} rows of no token")
+        return 1
+    if rows % T or not rows:
         raise ValueError(f"{name}: {rows} rows are not a whole number for each of {T} tokens")
-    return SkExperts(T, max(k, 1), E, K, N, _DTYPE[dtype])
+    return rows // T
 
 
-def _product_args(w, offsets, *index):
-    _typed(w, "weight", _HALF)
-    if w.dim() != 3:
-        raise ValueError(f"weight must be [E, N, K], got {list(w.shape)}")
-    _dev(offsets, "offsets", torch.int32), _shape(offsets, (w.shape[0] + 1,), "offsets")
-    _like(offsets, w, "offsets")
-    for t, n in index:
-        if t is not None:
-            _dev(t, n, torch.int32), _like(t, w, n)
-
-
-def _rows_2d(t, cols, ref, name):
+def _half_rows(t, name, cols, ref):
     _typed(t, name, _HALF)
     if t.dim() != 2 or t.shape[1] != cols:
         raise ValueError(f"{name} must have {cols} columns, got {list(t.shape)}")
     if t.dtype != ref.dtype:
-        raise TypeError(f"{name} must be {ref.dtype} as the weight, got {t.dtype}")
-    _like(t, ref, name)
+        raise TypeError(f"{name} must be {ref.dtype}, got {t.dtype}")
+    _match(t, name, ref)
 
 
-def sinkhorn_experts_forward(x, weight, offsets, tokens=None, stream=None):
+def _weight(w):
+    _typed(w, "weight", _HALF)
+    if w.dim() != 3:
+        raise ValueError(f"weight must be [E, N, K], got {list(w.shape)}")
+    return w.shape
+
+
+@_on_stream
+def sinkhorn_experts_forward(x, weight, offsets, tokens=None):
     """Rows of each expert times its matrix: y [R, N].  x [T, K] gathered through tokens [R], or, without tokens,
     x [R, K] in the rows' order; weight [E, N, K]; offsets [E + 1]."""
-    lib = load_library()
-    _product_args(weight, offsets, (tokens, "tokens"))
-    E, N, K = weight.shape
-    _rows_2d(x, K, weight, "x")
-    rows = x.shape[0] if tokens is None else tokens.numel()
-    p = _experts(rows, None if tokens is None else x.shape, weight.shape, offsets, tokens, x.dtype, "tokens")
-    with _on(stream):
-        y = torch.empty((rows, N), device=x.device, dtype=x.dtype)
-    _call(lib.sinkhorn_experts_forward, x.device, stream, ctypes.byref(p), _ptr(x), _ptr(weight), _ptr(offsets),
-          _ptr(tokens), _ptr(y))
+    E, N, K = _weight(weight)
+    _half_rows(x, "x", K, weight)
+    _match(offsets, "offsets", x, (E + 1,), torch.int32)
+    rows = T = x.shape[0]
+    k = 1
+    if tokens is not None:
+        _match(tokens, "tokens", x, None, torch.int32)
+        rows = tokens.numel()
+        k = _rows_of(rows, T, "tokens")
+    p, _ = _experts(T, k, E, K, N, _HALF[x.dtype])
+    y = torch.empty((rows, N), device=x.device, dtype=x.dtype)
+    _call(load_library().sinkhorn_experts_forward, x.device, p, x.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
+          _ptr(tokens), y.data_ptr())
     return y
 
 
-def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, stream=None, workspace=None):
+@_on_stream
+def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspace=None):
     """Gradient of x: [T, K] with slots [T, k], else that of the rows, [R, K]."""
-    lib = load_library()
-    _product_args(weight, offsets, (slots, "slots"))
-    E, N, K = weight.shape
-    _rows_2d(grad_y, N, weight, "grad_y")
-    rows = grad_y.shape[0]
-    if slots is not None and (slots.dim() != 2 or slots.numel() != rows):
-        raise ValueError(f"slots must be [T, k] with T k = {rows}, got {list(slots.shape)}")
-    p = _experts(rows, None if slots is None else slots.shape, weight.shape, offsets, slots, grad_y.dtype, "slots")
-    need = int(lib.sinkhorn_experts_workspace_bytes(ctypes.byref(p))) if slots is not None else 0
-    with _on(stream):
-        gx = torch.empty((p.T, K), device=grad_y.device, dtype=grad_y.dtype)
-        if need and (workspace is None or workspace.numel() < need):
-            workspace = torch.empty((need,), device=grad_y.device, dtype=torch.uint8)
-    _call(lib.sinkhorn_experts_backward_input, grad_y.device, stream, ctypes.byref(p), _ptr(grad_y), _ptr(weight),
-          _ptr(offsets), _ptr(slots), _ptr(gx), _ptr(workspace) if need else None, ctypes.c_size_t(need))
+    E, N, K = _weight(weight)
+    _half_rows(grad_y, "grad_y", N, weight)
+    _match(offsets, "offsets", grad_y, (E + 1,), torch.int32)
+    T, k, need = grad_y.shape[0], 1, 0
+    if slots is not None:
+        _match(slots, "slots", grad_y, None, torch.int32)
+        if slots.dim() != 2 or slots.numel() != T:
+            raise ValueError(f"slots must be [T, k] with T k = {T}, got {list(slots.shape)}")
+        T = slots.shape[0]
+        k = _rows_of(slots.numel(), T, "slots")
+    p, need = _experts(T, k, E, K, N, _HALF[grad_y.dtype])
+    gx = torch.empty((T, K), device=grad_y.device, dtype=grad_y.dtype)
+    scratch = None if slots is None else _scratch(workspace, need, grad_y.device)
+    _call(load_library().sinkhorn_experts_backward_input, grad_y.device, p, grad_y.data_ptr(), weight.data_ptr(),
+          offsets.data_ptr(), _ptr(slots), gx.data_ptr(), _ptr(scratch), need)
     return gx
 
 
-def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None, stream=None):
+@_on_stream
+def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None):
     """Gradient of the weight, [E, N, K]."""
-    lib = load_library()
-    _typed(grad_y, "grad_y", _HALF), _typed(x, "x", _HALF)
+    _typed(grad_y, "grad_y", _HALF)
     if grad_y.dim() != 2 or x.dim() != 2:
         raise ValueError("grad_y must be [R, N] and x [T, K] or [R, K]")
-    N, K = grad_y.shape[1], x.shape[1]
-    _dev(offsets, "offsets", torch.int32), _like(offsets, x, "offsets")
-    _rows_2d(grad_y, N, x, "grad_y")
-    rows = grad_y.shape[0]
+    (rows, N), (T, K) = grad_y.shape, x.shape
+    _half_rows(x, "x", K, grad_y)
+    _match(offsets, "offsets", x, None, torch.int32)
     E = offsets.numel() - 1
+    k = 1
     if tokens is not None:
-        _dev(tokens, "tokens", torch.int32), _shape(tokens, (rows,), "tokens"), _like(tokens, x, "tokens")
-    elif x.shape[0] != rows:
-        raise ValueError(f"without tokens x must have {rows} rows as grad_y, got {x.shape[0]}")
-    p = _experts(rows, None if tokens is None else x.shape, (E, N, K), offsets, tokens, x.dtype, "tokens")
-    with _on(stream):
-        gw = torch.empty((E, N, K), device=x.device, dtype=x.dtype)
-    _call(lib.sinkhorn_experts_backward_weight, x.device, stream, ctypes.byref(p), _ptr(grad_y), _ptr(x),
-          _ptr(offsets), _ptr(tokens), _ptr(gw))
+        _match(tokens, "tokens", x, (rows,), torch.int32)
+        k = _rows_of(rows, T, "tokens")
+    elif T != rows:
+        raise ValueError(f"without tokens x must have {rows} rows as grad_y, got {T}")
+    p, _ = _experts(T, k, E, K, N, _HALF[x.dtype])
+    gw = torch.empty((E, N, K), device=x.device, dtype=x.dtype)
+    _call(load_library().sinkhorn_experts_backward_weight, x.device, p, grad_y.data_ptr(), x.data_ptr(),
+          offsets.data_ptr(), _ptr(tokens), gw.data_ptr())
     return gw
 
 
@@ -269,117 +327,123 @@ def sinkhorn_expert_product(x, weight, offsets, tokens=None, slots=None):
     """Each expert's rows times its matrix, [R, N]; differentiable with respect to x and weight [E, N, K].
 
     With tokens [R] and slots [T, k] of a Routing, x is [T, K] and its rows are gathered; without both, x is [R, K],
-    in the rows' order.  Rows from offsets[E] on are zero."""
+    in the rows' order.  Rows from offsets[E] on are zero.  bfloat16 or float16, sums in 32 bits."""
     if (tokens is None) != (slots is None):
         raise ValueError("tokens and slots go together")
     x, weight = x.contiguous(), weight.contiguous()
-    if slots is not None:
-        if slots.dim() != 2 or slots.shape[0] != x.shape[0] or slots.numel() != tokens.numel():
-            raise ValueError(f"slots must be [T, k] with T = {x.shape[0]}, T k = {tokens.numel()}, "
-                             f"got {list(slots.shape)}")
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad):
+    if slots is not None and (slots.dim() != 2 or slots.shape[0] != x.shape[0] or slots.numel() != tokens.numel()):
+        raise ValueError(f"slots must be [T, k] with T = {x.shape[0]}, T k = {tokens.numel()}, "
+                         f"got {list(slots.shape)}")
+    if (x.requires_grad or weight.requires_grad) and torch.is_grad_enabled():
         return _ExpertProduct.apply(x, weight, offsets, tokens, slots)
     return sinkhorn_experts_forward(x, weight, offsets, tokens)
 
 
 # ---- dropout ----
 
-def _dropout(x, p, seed, offset, residual, stream=None):
-    lib = load_library()
-    _typed(x, "x")
-    if residual is not None:
-        _typed(residual, "residual", (x.dtype,)), _shape(residual, x.shape, "residual")
-        _like(residual, x, "residual")
-    args = _counter(p, seed, offset)
-    with _on(stream):
-        y = torch.empty_like(x)
-    _call(lib.sinkhorn_dropout, x.device, stream, x.numel(), _DTYPE[x.dtype], _ptr(x), _ptr(residual), _ptr(y), *args)
+def _run_dropout(x, residual, counter):
+    y = torch.empty_like(x)
+    _call(load_library().sinkhorn_dropout, x.device, x.numel(), _DTYPE[x.dtype], x.data_ptr(), _ptr(residual),
+          y.data_ptr(), *counter)
     return y
 
 
 class _Dropout(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, p, seed, offset):
-        ctx.p, ctx.seed, ctx.offset = p, seed, offset
-        return _dropout(x, p, seed, offset, residual)
+    def forward(ctx, x, residual, counter):
+        ctx.counter = counter
+        return _run_dropout(x, residual, counter)
 
     @staticmethod
     def backward(ctx, gy):
-        gx = _dropout(gy.contiguous(), ctx.p, ctx.seed, ctx.offset, None) if ctx.needs_input_grad[0] else None
-        return gx, gy if ctx.needs_input_grad[1] else None, None, None, None
+        gx = _run_dropout(gy.contiguous(), None, ctx.counter) if ctx.needs_input_grad[0] else None
+        return gx, gy if ctx.needs_input_grad[1] else None, None
 
 
-def sinkhorn_dropout(x, p, seed, offset=0, residual=None, stream=None):
+@_on_stream
+def sinkhorn_dropout(x, p, seed, offset=0, residual=None):
     """residual + dropout(x), differentiable with respect to x and residual.  An element is dropped with probability
     p (to 16 bits) by a generator keyed with seed (64 bits) and counted by offset (64 bits) and the element's number
     in x, so the mask is never stored: the same seed and offset drop the same elements.  A dropped element adds
     nothing, whatever it holds."""
     x = x.contiguous()
-    residual = None if residual is None else residual.contiguous()
-    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
-        if stream is not None:
-            raise ValueError("a differentiable call runs on the current stream")
-        return _Dropout.apply(x, residual, p, seed, offset)
-    return _dropout(x, p, seed, offset, residual, stream)
+    _typed(x, "x")
+    wants = x.requires_grad
+    if residual is not None:
+        residual = residual.contiguous()
+        _match(residual, "residual", x, x.shape, x.dtype)
+        wants = wants or residual.requires_grad
+    counter = _counter(p, seed, offset)
+    if wants and torch.is_grad_enabled():
+        return _Dropout.apply(x, residual, counter)
+    return _run_dropout(x, residual, counter)
 
 
 # ---- combination of expert rows ----
 
-def _combine_args(z, weights, slots):
+def _combine_sizes(z, weights, slots):
     _typed(z, "z")
-    _dev(slots, "slots", torch.int32), _like(slots, z, "slots")
+    _match(slots, "slots", z, None, torch.int32)
     if z.dim() != 2 or slots.dim() != 2 or z.shape[0] != slots.numel():
         raise ValueError(f"z must be [T k, D] and slots [T, k], got {list(z.shape)} {list(slots.shape)}")
-    _dev(weights, "weights"), _shape(weights, slots.shape, "weights"), _like(weights, z, "weights")
+    _match(weights, "weights", z, slots.shape, torch.float32)
     T, k = slots.shape
-    return SkCombine(T, z.shape[1], max(k, 1) if T == 0 else k, _DTYPE[z.dtype])
+    return T, z.shape[1], max(k, 1) if T == 0 else k
 
 
-def sinkhorn_combine_forward(z, weights, slots, residual=None, p=0.0, seed=0, offset=0, stream=None):
+@_on_stream
+def sinkhorn_combine_forward(z, weights, slots, residual=None, p=0.0, seed=0, offset=0):
     """y [T, D] = residual + dropout(sum_s weights[t, s] z[slots[t, s]])."""
-    lib = load_library()
-    c = _combine_args(z, weights, slots)
-    args = _counter(p, seed, offset)
+    T, D, k = _combine_sizes(z, weights, slots)
     if residual is not None:
-        _typed(residual, "residual", (z.dtype,)), _shape(residual, (c.T, c.D), "residual")
-        _like(residual, z, "residual")
-    with _on(stream):
-        y = torch.empty((c.T, c.D), device=z.device, dtype=z.dtype)
-    _call(lib.sinkhorn_combine_forward, z.device, stream, ctypes.byref(c), _ptr(z), _ptr(weights), _ptr(slots),
-          _ptr(residual), _ptr(y), *args)
+        _match(residual, "residual", z, (T, D), z.dtype)
+    return _run_combine(z, weights, slots, residual, T, D, k, _counter(p, seed, offset))
+
+
+def _run_combine(z, weights, slots, residual, T, D, k, counter):
+    y = torch.empty((T, D), device=z.device, dtype=z.dtype)
+    _call(load_library().sinkhorn_combine_forward, z.device, _combine(T, D, k, _DTYPE[z.dtype]), z.data_ptr(),
+          weights.data_ptr(), slots.data_ptr(), _ptr(residual), y.data_ptr(), *counter)
     return y
 
 
-def sinkhorn_combine_backward(z, weights, slots, offsets, grad_y, p=0.0, seed=0, offset=0, stream=None):
+@_on_stream
+def sinkhorn_combine_backward(z, weights, slots, offsets, grad_y, p=0.0, seed=0, offset=0):
     """(grad_z [T k, D], grad_weights [T, k]); offsets as from the router (its last entry: the rows in use)."""
-    lib = load_library()
-    c = _combine_args(z, weights, slots)
-    args = _counter(p, seed, offset)
-    _typed(grad_y, "grad_y", (z.dtype,)), _shape(grad_y, (c.T, c.D), "grad_y"), _like(grad_y, z, "grad_y")
-    _dev(offsets, "offsets", torch.int32), _like(offsets, z, "offsets")
-    with _on(stream):
-        gz = torch.empty_like(z)
-        gw = torch.empty_like(weights)
-    used = ctypes.c_void_p(offsets.data_ptr() + 4 * (offsets.numel() - 1))
-    _call(lib.sinkhorn_combine_backward, z.device, stream, ctypes.byref(c), _ptr(z), _ptr(weights), _ptr(slots), used,
-          _ptr(grad_y), _ptr(gz), _ptr(gw), *args)
+    T, D, k = _combine_sizes(z, weights, slots)
+    _match(grad_y, "grad_y", z, (T, D), z.dtype)
+    _used(offsets, z)
+    return _run_combine_backward(z, weights, slots, offsets, grad_y, T, D, k, _counter(p, seed, offset))
+
+
+def _used(offsets, z):
+    _match(offsets, "offsets", z, None, torch.int32)
+    if offsets.numel() < 1:
+        raise ValueError("offsets must be [E + 1]")
+
+
+def _run_combine_backward(z, weights, slots, offsets, grad_y, T, D, k, counter):
+    gz, gw = torch.empty_like(z), torch.empty_like(weights)
+    _call(load_library().sinkhorn_combine_backward, z.device, _combine(T, D, k, _DTYPE[z.dtype]), z.data_ptr(),
+          weights.data_ptr(), slots.data_ptr(), offsets.data_ptr() + 4 * (offsets.numel() - 1), grad_y.data_ptr(),
+          gz.data_ptr(), gw.data_ptr(), *counter)
     return gz, gw
 
 
 class _Combine(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, z, weights, slots, offsets, residual, p, seed, offset):
+    def forward(ctx, z, weights, slots, offsets, residual, sizes, counter):
         ctx.save_for_backward(z, weights, slots, offsets)
-        ctx.drop = (p, seed, offset)
-        return sinkhorn_combine_forward(z, weights, slots, residual, p, seed, offset)
+        ctx.call = (*sizes, counter)
+        return _run_combine(z, weights, slots, residual, *sizes, counter)
 
     @staticmethod
     def backward(ctx, gy):
         z, weights, slots, offsets = ctx.saved_tensors
         gz = gw = None
         if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
-            gz, gw = sinkhorn_combine_backward(z, weights, slots, offsets, gy.contiguous(), *ctx.drop)
-        return gz, gw, None, None, gy if ctx.needs_input_grad[4] else None, None, None, None
+            gz, gw = _run_combine_backward(z, weights, slots, offsets, gy.contiguous(), *ctx.call)
+        return gz, gw, None, None, gy if ctx.needs_input_grad[4] else None, None, None
 
 
 def sinkhorn_expert_combine(z, weights, slots, offsets, residual=None, p=0.0, seed=0, offset=0):
@@ -387,8 +451,14 @@ def sinkhorn_expert_combine(z, weights, slots, offsets, residual=None, p=0.0, se
     [T k, D], weights [T, k] and residual.  slots and offsets are a Routing's; p, seed and offset as in
     sinkhorn_dropout, over the elements of the result."""
     z, weights = z.contiguous(), weights.contiguous()
-    residual = None if residual is None else residual.contiguous()
-    if torch.is_grad_enabled() and (z.requires_grad or weights.requires_grad or
-                                    (residual is not None and residual.requires_grad)):
-        return _Combine.apply(z, weights, slots, offsets, residual, p, seed, offset)
-    return sinkhorn_combine_forward(z, weights, slots, residual, p, seed, offset)
+    T, D, k = sizes = _combine_sizes(z, weights, slots)
+    wants = z.requires_grad or weights.requires_grad
+    if residual is not None:
+        residual = residual.contiguous()
+        _match(residual, "residual", z, (T, D), z.dtype)
+        wants = wants or residual.requires_grad
+    counter = _counter(p, seed, offset)
+    if wants and torch.is_grad_enabled():
+        _used(offsets, z)
+        return _Combine.apply(z, weights, slots, offsets, residual, sizes, counter)
+    return _run_combine(z, weights, slots, residual, T, D, k, counter)
