@@ -371,7 +371,7 @@ typedef struct {
  *   balance  [1]           out  E sum_e f_e P_e with f_e = counts[e] / (k n),
  *                               P_e = mean of softmax(logits)_e over the live
  *   z_loss   [1]           out  mean of logsumexp(logits_t)^2 over the live
- *   state    [2 T + 1]     out  for the backward pass
+ *   state    [2 T + 1]     out  for the backward pass (may be NULL without one)
  * With n = 0 both losses are 0.  A NaN (or +inf) among a live token's logits
  * makes its weights and the losses NaN; masked tokens' logits are not used.
  * Deterministic (fixed order, no atomics).

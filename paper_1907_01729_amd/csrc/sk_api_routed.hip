@@ -81,7 +81,7 @@ sk_status sinkhorn_route_forward(const sk_router *r, const void *logits, const f
                                  void *workspace, size_t ws_bytes, void *stream) {
     const sk_status st = check_router(r);
     if (st != SK_OK) return st;
-    if (!counts || !offsets || !balance || !z_loss || !state) return SK_ERR_NULLPTR;
+    if (!counts || !offsets || !balance || !z_loss) return SK_ERR_NULLPTR;
     if (r->T > 0 && (!logits || !weights || !experts || !tokens || !slots)) return SK_ERR_NULLPTR;
     const size_t need = sk::route_workspace_bytes(r->T, r->E, r->k);
     if (ws_bytes < need) return SK_ERR_WORKSPACE;

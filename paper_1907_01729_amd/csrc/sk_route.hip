@@ -2,9 +2,9 @@
 // the order of the (token, slot) pairs by expert; and the gradient of the logits.
 //
 // A token's logits are held by a group of L lanes, V consecutive ones to a lane (E <= L V), so one read serves the
-// softmax, the k largest and the sums over tokens.  A group takes a run of consecutive tokens and keeps, in the
-// registers of the lane that holds an expert, how many pairs the expert has so far: that count is a pair's rank among
-// the run's pairs of that expert, so the order by (expert, token, slot) needs no sort and no atomics:
+// softmax, the k largest and the sums over tokens.  A group takes a run of consecutive tokens, one after the other, and
+// counts each expert's pairs in LDS as it goes: the count is a pair's rank among the run's pairs of that expert, so the
+// order by (expert, token, slot) needs no sort, and no two lanes count the same expert at a time:
 //   sk_route_tokens   one work-group per block of tokens; ranks within the block; counts, probability sums per block
 //   sk_route_scan     per expert, the blocks' counts summed into starts; totals
 //   sk_route_place    start of the expert + start of the block + rank; the losses
@@ -17,10 +17,13 @@ namespace sk {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kRowBcast15 = 0x142;  // DPP: lane 15 of a row of 16 to the next row
+constexpr int kRowBcast31 = 0x143;  // DPP: lane 31 to the upper 32
 constexpr int kMaxK = 16;
-constexpr int kMaxRun = 32;        // tokens of a group: ranks within a run stay below 2^16 and the pairs in LDS
-constexpr int kBlocksWanted = 512;  // two work-groups per CU
-constexpr int kScanCols = 16;
+constexpr int kMaxRun = 32;         // tokens of a group: ranks within a run stay below 2^16 and the pairs in LDS
+constexpr int kBlocksWanted = 512;
+constexpr int kManyThreads = 1024;
+constexpr uint32_t kNoPair = 0xFFFFFFFFu;
 
 // Reductions over aligned groups of L lanes; every lane of the group ends with the same bits.
 template <int L>
@@ -50,6 +53,18 @@ __device__ __forceinline__ float group_max(float v) {
         v = fmaxf(b.lo, b.hi);
     }
     return v;
+}
+// The group's largest value where only that is wanted: over a whole wavefront by broadcasts to its last lane and a scalar.
+template <int L>
+__device__ __forceinline__ float group_best(float v) {
+    if constexpr (L < 64) return group_max<L>(v);
+    v = max_q(v);
+    v = fmaxf(v, dpp<kRowRor8>(v));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), kRowBcast15, 0xA,
+                                                            0xF, false)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), kRowBcast31, 0xC,
+                                                            0xF, false)));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 // The group's bits of a wavefront's ballot.
 template <int L>
@@ -149,35 +164,36 @@ __device__ __forceinline__ void route_losses(const RouteArgs &A, float live, flo
         for (int q = 0; q < kThreads / 64; ++q) all += red[q];
         *A.balance = (float)A.E * all;
         *A.z_loss = z / n;
-        A.state[2 * (size_t)A.T] = live;
+        if (A.state) A.state[2 * (size_t)A.T] = live;
     }
 }
 
-// ONE: the only work-group; writes the order and the losses too.
-template <class T, int L, int V, bool VEC, bool ONE>
-__global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePlan P) {
-    constexpr int G = kThreads / L;
+// NT threads.  ONE: the only work-group; writes the order and the losses too.
+template <class T, int L, int V, bool VEC, bool ONE, int NT>
+__global__ __launch_bounds__(NT) void sk_route_tokens(RouteArgs A, RoutePlan P) {
+    constexpr int G = NT / L;
     extern __shared__ int32_t lds[];
     int32_t *cnt_lds = lds;                                      // [G][L V]
     float *prob_lds = reinterpret_cast<float *>(lds + G * L * V);  // [G][L V]
     uint32_t *pair = reinterpret_cast<uint32_t *>(prob_lds + G * L * V);  // [G][run][k]: expert << 16 | rank
-    __shared__ float z_lds[G], live_lds[G], red[kThreads / 64];
-    __shared__ int32_t off[ONE ? L * V + 1 : 1], wave_total[kThreads / 64];
+    __shared__ float z_lds[G], live_lds[G], red[NT / 64];
+    __shared__ int32_t off[ONE ? L * V + 1 : 1], wave_total[NT / 64];
 
     const int E = A.E, k = A.k;
     const int lane = threadIdx.x & (L - 1), g = threadIdx.x / L;
     const int first = lane * V;
     const int64_t t0 = ((int64_t)blockIdx.x * G + g) * P.run;
     uint32_t *mine = pair + (size_t)g * P.run * k;
+    int32_t *cnt = cnt_lds + g * L * V;  // pairs so far
 
     float bias[V], psum[V];
-    int32_t cnt[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         bias[v] = A.bias && first + v < E ? A.bias[first + v] : 0.f;
         psum[v] = 0.f;
-        cnt[v] = 0;
+        cnt[first + v] = 0;
     }
+    __builtin_amdgcn_wave_barrier();
     float zsum = 0.f, nlive = 0.f;
 
     for (int q = 0; q < P.run; ++q) {
@@ -219,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
             zsum += lse * lse;
             nlive += 1.f;
         }
-        if (here && lane == 0) {
+        if (here && lane == 0 && A.state) {
             A.state[2 * t] = live ? mx : neg_inf();
             A.state[2 * t + 1] = sum;
         }
@@ -231,36 +247,41 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
             const float s = x[v] + bias[v];
             sc[v] = live && first + v < E && s > neg_inf() ? s : neg_inf();
         }
-        int my_expert = -1;
-        float my_logit = neg_inf();
-        uint32_t my_pair = 0xFFFFFFFFu;
+        // Each lane keeps the first of its best scores at hand; the lane whose it is notes the expert in LDS and looks for
+        // its next.  Nothing goes between lanes but the maximum.
+        float m = sc[0];
+        int at = 0;
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (sc[v] > m) m = sc[v], at = v;
         for (int s = 0; s < k; ++s) {
-            float m = sc[0];
+            const float best = group_best<L>(m);
+            const uint64_t holders = group_ballot<L>(m == best && m > neg_inf());
+            const int owner = holders ? __builtin_ctzll(holders) : 0;
+            if (lane == owner) {
+                mine[q * k + s] = holders ? (uint32_t)(first + at) << 16 : kNoPair;
 #pragma unroll
-            for (int v = 1; v < V; ++v) m = fmaxf(m, sc[v]);
-            const float best = group_max<L>(m);
-            const bool some = best > neg_inf();
-            const int owner = some ? __builtin_ctzll(group_ballot<L>(m == best)) : 0;
-            uint32_t word = 0;
-            float logit = 0.f;
-            bool open = some && lane == owner;  // the owner's first score equal to the best is the one
+                for (int v = 0; v < V; ++v) sc[v] = v == at ? neg_inf() : sc[v];
+                m = sc[0], at = 0;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const bool hit = open && sc[v] == best;
-                word = hit ? (uint32_t)(first + v) << 16 | (uint32_t)cnt[v] : word;
-                logit = hit ? x[v] : logit;
-                cnt[v] += hit;
-                sc[v] = hit ? neg_inf() : sc[v];
-                open = open && !hit;
-            }
-            word = __shfl((int)word, owner, L);
-            logit = __shfl(logit, owner, L);
-            if (lane == s && some) {
-                my_expert = (int)(word >> 16);
-                my_logit = logit;
-                my_pair = word;
+                for (int v = 1; v < V; ++v)
+                    if (sc[v] > m) m = sc[v], at = v;
             }
         }
+        __builtin_amdgcn_wave_barrier();  // a wavefront's LDS operations complete in order
+        // lane s has slot s: its rank, its logit
+        int my_expert = -1;
+        float my_logit = neg_inf();
+        if (lane < k) {
+            uint32_t word = mine[q * k + lane];
+            if (word != kNoPair) {
+                my_expert = (int)(word >> 16);
+                my_logit = (float)static_cast<const T *>(A.logits)[t * (int64_t)E + my_expert];
+                word |= (uint32_t)atomicAdd(&cnt[my_expert], 1);
+                mine[q * k + lane] = word;
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
 
         // weights of the chosen: lane s has slot s
         float w = 0.f;
@@ -277,20 +298,16 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
         if (here && lane < k) {
             A.weights[t * k + lane] = w;
             A.experts[t * k + lane] = my_expert;
-            mine[q * k + lane] = my_pair;
         }
     }
 
     // The block's totals, and each group's start among them.
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        cnt_lds[g * L * V + first + v] = cnt[v];
-        prob_lds[g * L * V + first + v] = psum[v];
-    }
+    for (int v = 0; v < V; ++v) prob_lds[g * L * V + first + v] = psum[v];
     if (lane == 0) z_lds[g] = zsum, live_lds[g] = nlive;
     __syncthreads();
     const RouteSpace S = route_space(A.ws, P.blocks, E);
-    for (int e = threadIdx.x; e < E; e += kThreads) {
+    for (int e = threadIdx.x; e < E; e += NT) {
         int32_t c = 0;
         float p = 0.f;
         for (int q = 0; q < G; ++q) {
@@ -314,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
     if constexpr (ONE) {
         const int32_t *total = reinterpret_cast<const int32_t *>(prob_lds) + L * V;
         expert_offsets(E, off, wave_total, [&](int e) { return total[e]; });
-        for (int e = threadIdx.x; e <= E; e += kThreads) A.offsets[e] = off[e];
+        for (int e = threadIdx.x; e <= E; e += NT) A.offsets[e] = off[e];
         route_losses(A, live, z, red, [&](int e) { return total[e]; }, [&](int e) { return prob_lds[e]; });
     } else if (threadIdx.x == 0) {
         S.z[blockIdx.x] = z;
@@ -326,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
         if (at >= (int64_t)A.T * k) break;
         const uint32_t word = mine[q];
         int32_t slot = -1;
-        if (word != 0xFFFFFFFFu) {
+        if (word != kNoPair) {
             const int e = (int)(word >> 16);
             slot = cnt_lds[g * L * V + e] + (int32_t)(word & 0xFFFFu);
             if constexpr (ONE) {
@@ -337,15 +354,12 @@ __global__ __launch_bounds__(kThreads) void sk_route_tokens(RouteArgs A, RoutePl
         A.slots[at] = slot;  // !ONE: the rank within the block until sk_route_place
     }
     if constexpr (ONE)
-        for (int64_t r = off[E] + threadIdx.x; r < (int64_t)A.T * k; r += kThreads) A.tokens[r] = -1;
+        for (int64_t r = off[E] + threadIdx.x; r < (int64_t)A.T * k; r += NT) A.tokens[r] = -1;
 }
 
-// Work-groups of kScanCols experts: the blocks' counts become starts, in place; totals of counts and probabilities.
-// The last work-group sums z and the live tokens.
+// One wavefront an expert, its lanes a run of blocks each: the blocks' counts become starts, in place; totals of counts
+// and probabilities.  The last work-group sums z and the live tokens.
 __global__ __launch_bounds__(kThreads) void sk_route_scan(RouteArgs A, RoutePlan P) {
-    constexpr int N = kThreads / kScanCols;  // strands of a column
-    __shared__ int32_t c_lds[N][kScanCols];
-    __shared__ float p_lds[N][kScanCols];
     __shared__ float red[2][kThreads / 64];
     const RouteSpace S = route_space(A.ws, P.blocks, A.E);
     if (blockIdx.x + 1 == gridDim.x) {
@@ -361,33 +375,45 @@ __global__ __launch_bounds__(kThreads) void sk_route_scan(RouteArgs A, RoutePlan
         }
         return;
     }
-    const int col = threadIdx.x % kScanCols, strand = threadIdx.x / kScanCols;
-    const int e = blockIdx.x * kScanCols + col;
-    const int per = (P.blocks + N - 1) / N;
-    const int b0 = min(strand * per, P.blocks), b1 = min(b0 + per, P.blocks);
+    constexpr int kAtOnce = 8;  // loads under way together
+    const int lane = threadIdx.x & 63, e = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (e >= A.E) return;
+    const int per = (P.blocks + 63) / 64;
+    const int b0 = min(lane * per, P.blocks), b1 = min(b0 + per, P.blocks);
     int32_t c = 0;
     float p = 0.f;
-    if (e < A.E)
-        for (int b = b0; b < b1; ++b) {
-            c += S.cnt[(size_t)b * A.E + e];
-            p += S.prob[(size_t)b * A.E + e];
+    for (int b = b0; b < b1; b += kAtOnce) {
+        int32_t n[kAtOnce];
+        float f[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            n[i] = b + i < b1 ? S.cnt[(size_t)(b + i) * A.E + e] : 0;
+            f[i] = b + i < b1 ? S.prob[(size_t)(b + i) * A.E + e] : 0.f;
         }
-    c_lds[strand][col] = c;
-    p_lds[strand][col] = p;
-    __syncthreads();
-    if (e >= A.E) return;
-    int32_t start = 0;
-    for (int q = 0; q < strand; ++q) start += c_lds[q][col];
-    if (strand == 0) {
-        for (int q = 1; q < N; ++q) c += c_lds[q][col], p += p_lds[q][col];
-        A.counts[e] = c;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) c += n[i], p += f[i];
+    }
+    int32_t upto = c;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t up = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += up;
+    }
+    p = wave_sum(p);
+    if (lane == 63) {
+        A.counts[e] = upto;
         S.prob_all[e] = p;
     }
-    for (int b = b0; b < b1; ++b) {
-        int32_t *at = S.cnt + (size_t)b * A.E + e;
-        const int32_t n = *at;
-        *at = start;
-        start += n;
+    int32_t start = upto - c;
+    for (int b = b0; b < b1; b += kAtOnce) {
+        int32_t n[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) n[i] = b + i < b1 ? S.cnt[(size_t)(b + i) * A.E + e] : 0;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (b + i < b1) S.cnt[(size_t)(b + i) * A.E + e] = start;
+            start += n[i];
+        }
     }
 }
 
@@ -512,18 +538,25 @@ hipError_t with_shape(int E, bool vec, F f) {
     return f(Int<64>{}, Int<16>{}, std::false_type{});
 }
 
-// One block while each group has at most four tokens: two more launches take longer than those in turn.
+// One block while each group has at most four tokens: two more launches take longer than those in turn.  Beyond, up to
+// 512 blocks, of 1024 threads where 256 would leave a SIMD fewer than eight wavefronts (the k rounds of maxima are one
+// chain of latencies): more blocks would be as many more partial sums for the scan.  65536 tokens, 256 experts, k = 8:
+// 118 us with 512 blocks of 256 threads; with 2048 of them 80 us, but 34 us of scan against 14.
 RoutePlan route_plan(int T, int E) {
     RoutePlan P;
-    P.groups = kThreads / group_lanes(E);
+    const int L = group_lanes(E);
+    P.groups = kThreads / L;
     if (T <= 4 * P.groups) {
         P.run = T > 0 ? (T + P.groups - 1) / P.groups : 1;
         P.blocks = 1;
         return P;
     }
+    if (E <= 256 && T > kBlocksWanted * P.groups) P.groups = kManyThreads / L;
     const int64_t wanted = (int64_t)kBlocksWanted * P.groups;
+    // the pairs of a work-group of 1024 threads: at most 16 KB of LDS
+    const int most = P.groups * L == kManyThreads ? kMaxRun * L / 128 : kMaxRun;
     int64_t run = (T + wanted - 1) / wanted;
-    P.run = (int)(run > kMaxRun ? kMaxRun : run);
+    P.run = (int)(run > most ? most : run);
     const int per = P.groups * P.run;
     P.blocks = (int)(((int64_t)T + per - 1) / per);
     return P;
@@ -549,17 +582,20 @@ hipError_t launch_route_forward(const RouteArgs &a, hipStream_t st) {
         return with_shape(a.E, vector_rows(a.logits, a.E, a.dtype), [&](auto l, auto v, auto vec) {
             constexpr int L = decltype(l)::value, V = decltype(v)::value;
             constexpr bool VEC = decltype(vec)::value;
-            const size_t lds = (size_t)(kThreads / L) * (2 * L * V + (size_t)P.run * a.k) * 4;
-            if (P.blocks == 1)
-                hipLaunchKernelGGL((sk_route_tokens<T, L, V, VEC, true>), dim3(1), dim3(kThreads), lds, st, a, P);
-            else
-                hipLaunchKernelGGL((sk_route_tokens<T, L, V, VEC, false>), dim3(P.blocks), dim3(kThreads), lds, st, a,
-                                   P);
-            return hipGetLastError();
+            const size_t lds = (size_t)P.groups * (2 * L * V + (size_t)P.run * a.k) * 4;
+            auto go = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3(P.blocks), dim3(P.groups * L), lds, st, a, P);
+                return hipGetLastError();
+            };
+            if (P.blocks == 1) return go(sk_route_tokens<T, L, V, VEC, true, kThreads>);
+            if constexpr (V <= 4) {
+                if (P.groups * L == kManyThreads) return go(sk_route_tokens<T, L, V, VEC, false, kManyThreads>);
+            }
+            return go(sk_route_tokens<T, L, V, VEC, false, kThreads>);
         });
     });
     if (err != hipSuccess || P.blocks == 1) return err;
-    hipLaunchKernelGGL(sk_route_scan, dim3((a.E + kScanCols - 1) / kScanCols + 1), dim3(kThreads), 0, st, a, P);
+    hipLaunchKernelGGL(sk_route_scan, dim3((a.E + kThreads / 64 - 1) / (kThreads / 64) + 1), dim3(kThreads), 0, st, a, P);
     const int64_t pairs = (int64_t)a.T * a.k;
     int64_t grid = (pairs + 4 * kThreads - 1) / (4 * kThreads);
     if (grid > 1024) grid = 1024;

@@ -130,6 +130,10 @@ def _counter(p, seed, offset):
 def sinkhorn_route_forward(logits, k, bias=None, mask=None, renormalize=True, workspace=None):
     """logits [T, E] float32, bfloat16 or float16; bias [E] float32; mask [T] bool (False: no token).
     Returns (Routing, state); state goes to sinkhorn_route_backward.  stream=: as in sinkhorn_forward."""
+    return _route_forward(logits, k, bias, mask, renormalize, True, workspace)
+
+
+def _route_forward(logits, k, bias, mask, renormalize, with_state, workspace=None):
     _typed(logits, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must be [T, E], got {list(logits.shape)}")
@@ -145,11 +149,12 @@ def sinkhorn_route_forward(logits, k, bias=None, mask=None, renormalize=True, wo
     weights, experts, slots = torch.empty((T, n), **real), torch.empty((T, n), **whole), torch.empty((T, n), **whole)
     tokens, counts, offsets = (torch.empty((T * n,), **whole), torch.empty((E,), **whole),
                                torch.empty((E + 1,), **whole))
-    balance, z, state = torch.empty((), **real), torch.empty((), **real), torch.empty((2 * T + 1,), **real)
+    balance, z = torch.empty((), **real), torch.empty((), **real)
+    state = torch.empty((2 * T + 1,), **real) if with_state else None
     scratch = _scratch(workspace, need, dev)
     _call(load_library().sinkhorn_route_forward, dev, r, logits.data_ptr(), _ptr(bias), _ptr(mask),
           weights.data_ptr(), experts.data_ptr(), counts.data_ptr(), offsets.data_ptr(), tokens.data_ptr(),
-          slots.data_ptr(), balance.data_ptr(), z.data_ptr(), state.data_ptr(), _ptr(scratch), need)
+          slots.data_ptr(), balance.data_ptr(), z.data_ptr(), _ptr(state), _ptr(scratch), need)
     return Routing(weights, experts, counts, offsets, tokens, slots, balance, z), state
 
 
@@ -189,7 +194,7 @@ def _contiguous(g):
 class _Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, bias, mask, renormalize):
-        r, state = sinkhorn_route_forward(logits, k, bias, mask, renormalize)
+        r, state = _route_forward(logits, k, bias, mask, renormalize, True)
         ctx.save_for_backward(logits, r.weights, r.experts, r.counts, state)
         ctx.k, ctx.renormalize = int(k), renormalize
         ctx.mark_non_differentiable(r.experts, r.counts, r.offsets, r.tokens, r.slots)
@@ -212,7 +217,7 @@ def sinkhorn_route(logits, k, bias=None, mask=None, renormalize=True) -> Routing
     mask = None if mask is None else mask.contiguous()
     if logits.requires_grad and torch.is_grad_enabled():
         return Routing(*_Route.apply(logits, k, bias, mask, renormalize))
-    return sinkhorn_route_forward(logits, k, bias, mask, renormalize)[0]
+    return _route_forward(logits, k, bias, mask, renormalize, False)[0]
 
 
 # ---- experts' products ----

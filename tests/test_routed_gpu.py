@@ -588,3 +588,9 @@ def test_refusals_of_gpu_tensors():
         sk.sinkhorn_expert_combine(z, r.weights, r.slots, r.offsets, residual=x[:, :63])
     with pytest.raises(TypeError):
         sk.sinkhorn_expert_combine(z, r.weights, r.slots.long(), r.offsets)
+
+
+@pytest.mark.parametrize("T,E,k", [(2500, 256, 8), (4500, 100, 4), (9000, 40, 2), (17000, 6, 2)])
+def test_route_work_groups_of_many_threads(T, E, k):
+    """Enough tokens for work-groups of 1024 threads, at each number of lanes to a token."""
+    check_route(make_logits(T, E, BF16, T), k, mask=torch.rand(T, generator=gen(T)) < 0.9)
