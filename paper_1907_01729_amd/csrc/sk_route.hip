@@ -54,17 +54,33 @@ __device__ __forceinline__ float group_max(float v) {
     }
     return v;
 }
-// The group's largest value where only that is wanted: over a whole wavefront by broadcasts to its last lane and a scalar.
+// The largest key of a group.  Keys are whole numbers (the larger of two floats costs two instructions more, which make
+// NaN quiet); over a whole wavefront by broadcasts to its last lane and a scalar.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t key_dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
 template <int L>
-__device__ __forceinline__ float group_best(float v) {
-    if constexpr (L < 64) return group_max<L>(v);
-    v = max_q(v);
-    v = fmaxf(v, dpp<kRowRor8>(v));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), kRowBcast15, 0xA,
-                                                            0xF, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), kRowBcast31, 0xC,
-                                                            0xF, false)));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+__device__ __forceinline__ uint32_t group_best(uint32_t v) {
+    v = max(v, key_dpp<kQuadXor1>(v));
+    v = max(v, key_dpp<kQuadXor2>(v));
+    v = max(v, key_dpp<kHalfMirror>(v));
+    if constexpr (L >= 16) v = max(v, key_dpp<kRowRor8>(v));
+    if constexpr (L == 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max((uint32_t)r[0], (uint32_t)r[1]);
+    }
+    if constexpr (L == 64) {
+        v = max(v, key_dpp<kRowBcast15, 0xA>(v));
+        v = max(v, key_dpp<kRowBcast31, 0xC>(v));
+        v = (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    }
+    return v;
+}
+// Keys in the order of the scores, above 0; 0: not to be taken (-inf, NaN).  -0 and 0 are the same.
+__device__ __forceinline__ uint32_t score_key(float s) {
+    const uint32_t u = __float_as_uint(s + 0.f);
+    return s > neg_inf() ? u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u) : 0u;
 }
 // The group's bits of a wavefront's ballot.
 template <int L>
@@ -241,31 +257,28 @@ __global__ __launch_bounds__(NT) void sk_route_tokens(RouteArgs A, RoutePlan P) 
         }
 
         // the k largest scores, ties to the lowest expert; scores of -inf and NaN are not taken
-        float sc[V];
+        uint32_t key[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float s = x[v] + bias[v];
-            sc[v] = live && first + v < E && s > neg_inf() ? s : neg_inf();
-        }
+        for (int v = 0; v < V; ++v) key[v] = live && first + v < E ? score_key(x[v] + bias[v]) : 0u;
         // Each lane keeps the first of its best scores at hand; the lane whose it is notes the expert in LDS and looks for
         // its next.  Nothing goes between lanes but the maximum.
-        float m = sc[0];
+        uint32_t m = 0;
         int at = 0;
+        auto look = [&] {
+            m = key[0], at = 0;
 #pragma unroll
-        for (int v = 1; v < V; ++v)
-            if (sc[v] > m) m = sc[v], at = v;
+            for (int v = 1; v < V; ++v)
+                if (key[v] > m) m = key[v], at = v;
+        };
+        look();
         for (int s = 0; s < k; ++s) {
-            const float best = group_best<L>(m);
-            const uint64_t holders = group_ballot<L>(m == best && m > neg_inf());
-            const int owner = holders ? __builtin_ctzll(holders) : 0;
-            if (lane == owner) {
-                mine[q * k + s] = holders ? (uint32_t)(first + at) << 16 : kNoPair;
+            const uint32_t best = group_best<L>(m);
+            const uint64_t holders = group_ballot<L>(m == best);
+            if (lane == __builtin_ctzll(holders)) {
+                mine[q * k + s] = best ? (uint32_t)(first + at) << 16 : kNoPair;
 #pragma unroll
-                for (int v = 0; v < V; ++v) sc[v] = v == at ? neg_inf() : sc[v];
-                m = sc[0], at = 0;
-#pragma unroll
-                for (int v = 1; v < V; ++v)
-                    if (sc[v] > m) m = sc[v], at = v;
+                for (int v = 0; v < V; ++v) key[v] = v == at ? 0u : key[v];
+                look();
             }
         }
         __builtin_amdgcn_wave_barrier();  // a wavefront's LDS operations complete in order
