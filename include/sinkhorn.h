@@ -425,11 +425,15 @@ SK_API sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void
                                                  const int32_t *offsets, const int32_t *slots, void *grad_x,
                                                  void *workspace, size_t ws_bytes, void *stream);
 
-/* Gradient of w [E, N, K]: sum_r grad_y[r]^T x[src(r)] over each expert's rows
- * (0 for an expert without rows). */
+/*
+ * Gradient of w [E, N, K]: sum_r grad_y[r]^T x[src(r)] over each expert's rows
+ * (0 for an expert without rows).  Few small matrices over many rows are
+ * summed in parts, which need a workspace.
+ */
+SK_API size_t sinkhorn_experts_weight_workspace_bytes(const sk_experts *p);
 SK_API sk_status sinkhorn_experts_backward_weight(const sk_experts *p, const void *grad_y, const void *x,
                                                   const int32_t *offsets, const int32_t *tokens, void *grad_w,
-                                                  void *stream);
+                                                  void *workspace, size_t ws_bytes, void *stream);
 
 /*
  * Dropout from a counter-based generator, on top of a residual:

@@ -46,6 +46,7 @@ EXPORTED = (
     "sinkhorn_experts_forward",
     "sinkhorn_experts_workspace_bytes",
     "sinkhorn_experts_backward_input",
+    "sinkhorn_experts_weight_workspace_bytes",
     "sinkhorn_experts_backward_weight",
     "sinkhorn_dropout",
     "sinkhorn_combine_forward",
@@ -138,7 +139,9 @@ def load_library():
     lib.sinkhorn_experts_workspace_bytes.argtypes = [PE]
     lib.sinkhorn_experts_workspace_bytes.restype = Z
     lib.sinkhorn_experts_backward_input.argtypes = [PE, P, P, P, P, P, P, Z, P]
-    lib.sinkhorn_experts_backward_weight.argtypes = [PE, P, P, P, P, P, P]
+    lib.sinkhorn_experts_weight_workspace_bytes.argtypes = [PE]
+    lib.sinkhorn_experts_weight_workspace_bytes.restype = Z
+    lib.sinkhorn_experts_backward_weight.argtypes = [PE, P, P, P, P, P, P, Z, P]
     lib.sinkhorn_dropout.argtypes = [ctypes.c_int64, I, P, P, P, D, U, U, P]
     lib.sinkhorn_combine_forward.argtypes = [PC, P, P, P, P, P, D, U, U, P]
     lib.sinkhorn_combine_backward.argtypes = [PC, P, P, P, P, P, P, P, D, U, U, P]

@@ -228,20 +228,28 @@ sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_
     return status_of(sk::launch_experts_input(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
+size_t sinkhorn_experts_weight_workspace_bytes(const sk_experts *p) {
+    if (check_experts(p) != SK_OK) return 0;
+    return sk::experts_weight_workspace_bytes(expert_args(p));
+}
+
 sk_status sinkhorn_experts_backward_weight(const sk_experts *p, const void *grad_y, const void *x,
                                            const int32_t *offsets, const int32_t *tokens, void *grad_w,
-                                           void *stream) {
+                                           void *workspace, size_t ws_bytes, void *stream) {
     const sk_status st = check_experts(p);
     if (st != SK_OK) return st;
     if (!offsets || !grad_w) return SK_ERR_NULLPTR;
     if (p->T > 0 && (!grad_y || !x)) return SK_ERR_NULLPTR;
     sk::ExpertArgs a = expert_args(p);
+    const size_t need = sk::experts_weight_workspace_bytes(a);
+    if (ws_bytes < need) return SK_ERR_WORKSPACE;
+    if (need && !workspace) return SK_ERR_NULLPTR;
     a.gy = grad_y;
     a.x = x;
     a.offsets = offsets;
     a.tokens = tokens;
     a.out = grad_w;
-    return status_of(sk::launch_experts_weight(a, static_cast<hipStream_t>(stream)));
+    return status_of(sk::launch_experts_weight(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

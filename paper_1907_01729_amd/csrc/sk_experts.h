@@ -15,11 +15,13 @@ struct ExpertArgs {
     void *out;
     float *out32;  // where set, the rows' result in 32 bits goes here instead
     int T, k, E, K, N, dtype;
+    int parts;  // weight: parts of the rows
 };
 size_t experts_workspace_bytes(int T, int k, int K);
+size_t experts_weight_workspace_bytes(const ExpertArgs &a);
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st);
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st);
-hipError_t launch_experts_weight(const ExpertArgs &a, hipStream_t st);
+hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st);
 
 template <class T>
 using Frag8 = T __attribute__((ext_vector_type(8)));

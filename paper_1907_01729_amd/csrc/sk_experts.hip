@@ -140,7 +140,7 @@ struct Operand {
 
 // GATHERED: x's rows are looked up in tokens.  WIDE: x has 2^32 bytes or more.
 template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE>
-__global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void sk_experts_tile(ExpertArgs A) {
+__global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void sk_experts_tile(ExpertArgs A) {
     constexpr int WAVES = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
     using OpA = Operand<T, MODE == kWeight, BM, WAVES, FM>;
     using OpB = Operand<T, MODE != kForward, BN, WAVES, FN>;
@@ -154,18 +154,22 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2, 
 
     // The tile: rows [m0, m1) of the result, columns from c0, of expert e, with `deep` products to a sum (weight: over
     // the rows from r0).
-    int e, m0, m1, c0, deep, r0 = 0;
+    int e, m0, m1, c0, deep, r0 = 0, part = 0;
     if constexpr (MODE == kWeight) {
         const int tn = (N + BM - 1) / BM, tk = (K + BN - 1) / BN;
-        const int t = xcd_order(blockIdx.x, A.E * tn * tk);
+        const int t = xcd_order(blockIdx.x, A.E * tn * tk * A.parts);
         if (t < 0) return;
-        e = t / (tn * tk);
-        const int i = t - e * (tn * tk);
+        const int tile = t / A.parts;
+        part = t - tile * A.parts;
+        e = tile / (tn * tk);
+        const int i = tile - e * (tn * tk);
         m0 = i / tk * BM, m1 = N;
         c0 = i % tk * BN;
+        // this part's share of the expert's rows, in whole steps
         const RowRange rr = expert_rows(A, e);
-        r0 = rr.begin;
-        deep = rr.end - rr.begin;
+        const int steps = (rr.end - rr.begin + kDeep - 1) / kDeep, share = (steps + A.parts - 1) / A.parts * kDeep;
+        r0 = min(rr.begin + part * share, rr.end);
+        deep = min(share, rr.end - r0);
     } else {
         const Tile t = find_tile(A, BM, (cols + BN - 1) / BN, blockIdx.x);
         if (t.expert < 0) return;
@@ -335,12 +339,12 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < FM; ++i) {
         const int row = m0 + wm + i * 16 + (lane & 15);
         if (row >= m1) continue;
-        const int64_t base = (MODE == kWeight ? (int64_t)e * N + row : row) * (int64_t)cols;
+        const int64_t base = (MODE == kWeight ? ((int64_t)part * A.E + e) * N + row : row) * (int64_t)cols;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const int col = c0 + wn + j * 16 + (lane >> 4) * 4;
             if (col >= cols) continue;
-            if (MODE == kInput && A.out32) {
+            if (MODE != kForward && A.out32) {
                 *reinterpret_cast<f32x4 *>(A.out32 + base + col) = acc[i][j];
             } else {
                 typedef T T4 __attribute__((ext_vector_type(4)));
@@ -351,6 +355,74 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2, 
             }
         }
     }
+}
+
+// ---- few rows: single tokens ----
+//
+// Forward for up to 16 rows of an expert at a time: what counts is that the weights are read at the memory's rate, so
+// many wavefronts have to ask for them at once.  A work-group takes kFewCols columns, and its four wavefronts a quarter
+// of the contraction each, straight from memory to registers; their sums meet in LDS.  A lane's 32 bytes of a row's 128
+// are two fragments: the products' order along the contraction is free as long as both factors have the same.
+
+constexpr int kFewRows = 16, kFewCols = 32, kFewChunk = 64, kFewAtOnce = 4;
+
+template <class T, bool GATHERED>
+__global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
+    constexpr int NC = kFewCols / 16, kWaves = kThreads / 64, kPitch = kFewCols + 4;
+    __shared__ __attribute__((aligned(16))) float part[kWaves][kFewRows][kPitch];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int K = A.K, N = A.N;
+    const Tile t = find_tile(A, kFewRows, (N + kFewCols - 1) / kFewCols, blockIdx.x);
+    if (t.expert < 0) return;
+    const int c0 = t.column * kFewCols, row = min(t.begin + (lane & 15), t.end - 1);
+    f32x4 acc[NC] = {};
+    if (t.expert < A.E) {
+        int64_t from = row;
+        if (GATHERED) {
+            const int token = A.tokens[row];
+            from = token >= 0 && token < A.T ? token : 0;
+        }
+        const int mine = (lane >> 4) * 16;  // the lane's first element of a chunk
+        const T *x = static_cast<const T *>(A.x) + from * K + mine;
+        const T *w[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+            w[j] = static_cast<const T *>(A.w) + ((int64_t)t.expert * N + min(c0 + j * 16 + (lane & 15), N - 1)) * K + mine;
+        const int chunks = (K + kFewChunk - 1) / kFewChunk;
+        for (int first = wave; first < chunks; first += kWaves * kFewAtOnce) {
+            Frag8<T> fx[kFewAtOnce][2], fw[kFewAtOnce][NC][2];
+#pragma unroll
+            for (int i = 0; i < kFewAtOnce; ++i) {
+                const int d = (first + i * kWaves) * kFewChunk;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool in = d + mine + h * 8 < K;
+                    fx[i][h] = in ? *reinterpret_cast<const Frag8<T> *>(x + d + h * 8) : Frag8<T>{};
+#pragma unroll
+                    for (int j = 0; j < NC; ++j)
+                        fw[i][j][h] = in ? *reinterpret_cast<const Frag8<T> *>(w[j] + d + h * 8) : Frag8<T>{};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kFewAtOnce; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NC; ++j) acc[j] = mfma16<T>(fw[i][j][h], fx[i][h], acc[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+        *reinterpret_cast<f32x4 *>(&part[wave][lane & 15][j * 16 + (lane >> 4) * 4]) = acc[j];
+    __syncthreads();
+    const int r = threadIdx.x / (kFewCols / 2), c = threadIdx.x % (kFewCols / 2) * 2;
+    if (t.begin + r >= t.end || c0 + c >= N) return;
+    float sum[2] = {};
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) sum[0] += part[q][r][c], sum[1] += part[q][r][c + 1];
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const T2 out = {(T)sum[0], (T)sum[1]};
+    *reinterpret_cast<T2 *>(static_cast<T *>(A.out) + (int64_t)(t.begin + r) * N + c0 + c) = out;
 }
 
 // ---- any sizes and alignment: 64 x 64 tiles, elements loaded one by one ----
@@ -488,35 +560,66 @@ __global__ __launch_bounds__(kThreads) void sk_experts_sum_slots(ExpertArgs A, c
     }
 }
 
+// The parts of a weight gradient, summed in order; n elements, a multiple of eight, eight to a thread.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sk_experts_sum_parts(const float *part, T *out, int64_t n, int parts) {
+    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8;
+    if (i >= n) return;
+    float sum[8] = {};
+    for (int q = 0; q < parts; ++q) {
+        float v[8];
+        load8(part + q * n + i, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    }
+    store8(out + i, sum);
+}
+
 template <class F>
 hipError_t with_half(int dtype, F f) {
     return dtype == SK_BF16 ? f(__bf16{}) : f(_Float16{});
 }
+
+int64_t parts_of(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
 // Row tiles that E experts' rows and the rows of none can take at most.
 int64_t most_row_tiles(const ExpertArgs &a, int tile) {
     const int64_t rows = (int64_t)a.T * a.k;
     return rows / tile + (rows < a.E + 1 ? rows : a.E + 1);
 }
-int64_t parts(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-template <int MODE, int BM, int BN, int WM, int WN>
-hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
-    const int64_t tiles = MODE == kWeight ? a.E * parts(a.N, BM) * parts(a.K, BN)
-                                          : most_row_tiles(a, BM) * parts(MODE == kForward ? a.N : a.K, BN);
-    return with_half(a.dtype, [&](auto type) {
-        using T = decltype(type);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(parts(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
-            return hipGetLastError();
-        };
-        if constexpr (MODE != kInput) {
-            if (a.tokens && (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32))
-                return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, true, true>);
-            if (a.tokens) return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, true, false>);
-        }
-        return go(sk_experts_tile<T, MODE, BM, BN, WM, WN, false, false>);
-    });
+// How a product is cut: tiles of `tile` squared, the weight gradient's rows in `parts`.
+struct Cut {
+    int tile, parts;
+};
+
+// Rows' products.  The expected number of tiles (half a tile of each expert is empty) decides.  256: one work-group a
+// CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each other's first
+// copies and last writes.  64: too few tiles of 128 to go round.  Measured, 256 / 128 / 64, in us: 65536 rows of 64
+// experts of 2048 x 2048 (9.0 rounds) 600 / 620 / -; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 169 / 157 / 217; 8000
+// rows of 2 of 2048 x 1024 (1.0) 39 / 45 / 64; 2331 rows of 12 of 520 x 1000 25 / 12.5 / 11.3; 300 rows of 2 of
+// 2048 x 2048 43 / 18.5 / 12.4.
+Cut cut_rows(const ExpertArgs &a, int cols) {
+    const int64_t rows = (int64_t)a.T * a.k;
+    auto tiles = [&](int64_t tile) { return (rows / tile + (a.E + 1) / 2) * parts_of(cols, tile); };
+    const int64_t large = tiles(256), rounds = parts_of(large, 256);
+    if (large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1};
+    return {tiles(128) >= 256 ? 128 : 64, 1};
+}
+
+// Weight gradients.  256 where there are two rounds of it and its edges waste no more than 128's would; else 128, or 64
+// for narrow matrices.  Few tiles over many rows are cut along the rows, into parts of eight steps or more, until there
+// are two work-groups a CU.  Measured, whole / in parts: 65536 rows of 16 experts of 512 x 512 118 / 76 us, 32768 rows
+// of 2 of 128 x 128 198 / 20.5 us; 256 / 128: 8192 rows of 8 of 4096 x 2048 221 / 248 us, 10308 rows of 28 of 272 x 1592
+// 46 / 41 us.
+Cut cut_weight(const ExpertArgs &a) {
+    auto tiles = [&](int64_t tile) { return a.E * parts_of(a.N, tile) * parts_of(a.K, tile); };
+    if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1};
+    const int tile = a.N <= 64 || a.K <= 64 ? 64 : 128;
+    const int64_t n = tiles(tile), steps = parts_of((int64_t)a.T * a.k, (int64_t)a.E * kDeep);
+    int64_t parts = parts_of(512, n);
+    if (parts > steps / 8) parts = steps / 8;
+    return {tile, (int)(parts < 1 ? 1 : parts)};
 }
 
 // Whether rows can be copied in chunks of 16 bytes.
@@ -525,38 +628,87 @@ bool chunks(const ExpertArgs &a) {
            (!a.gy || aligned16(a.gy)) && aligned16(a.out) && aligned16(a.out32);
 }
 
-template <int MODE>
-hipError_t launch_product(const ExpertArgs &a, hipStream_t st) {
-    if (chunks(a)) {
-        const int64_t rows = (int64_t)a.T * a.k;
-        const int64_t m = MODE == kWeight ? a.N : rows / a.E, c = MODE == kForward ? a.N : a.K;
-        if (m > 128 && c > 128) return launch_tile<MODE, 256, 256, 2, 4>(a, st);
-        return launch_tile<MODE, 128, 128, 2, 2>(a, st);
-    }
-    const int64_t cols = parts(MODE == kForward ? a.N : a.K, kAnyTile);
-    const int64_t grid = cols * (MODE == kWeight ? a.E * parts(a.N, kAnyTile) : most_row_tiles(a, kAnyTile));
+template <int MODE, int TILE, int WM, int WN>
+hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
+    const int64_t tiles = MODE == kWeight ? a.E * parts_of(a.N, TILE) * parts_of(a.K, TILE) * a.parts
+                                          : most_row_tiles(a, TILE) * parts_of(MODE == kForward ? a.N : a.K, TILE);
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
-        hipLaunchKernelGGL((sk_experts_any<T, MODE>), dim3((unsigned)(parts(grid, 8) * 8)), dim3(kThreads), 0, st, a);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(parts_of(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
+            return hipGetLastError();
+        };
+        if constexpr (MODE != kInput) {
+            if (a.tokens && (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32))
+                return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, true, true>);
+            if (a.tokens) return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, true, false>);
+        }
+        return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false>);
+    });
+}
+
+hipError_t launch_few(const ExpertArgs &a, hipStream_t st) {
+    const int64_t tiles = most_row_tiles(a, kFewRows) * parts_of(a.N, kFewCols);
+    return with_half(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        const dim3 grid((unsigned)(parts_of(tiles, 8) * 8));
+        if (a.tokens)
+            hipLaunchKernelGGL((sk_experts_few<T, true>), grid, dim3(kThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL((sk_experts_few<T, false>), grid, dim3(kThreads), 0, st, a);
         return hipGetLastError();
     });
+}
+
+template <int MODE>
+hipError_t launch_any(const ExpertArgs &a, hipStream_t st) {
+    const int64_t cols = parts_of(MODE == kForward ? a.N : a.K, kAnyTile);
+    const int64_t grid = cols * (MODE == kWeight ? a.E * parts_of(a.N, kAnyTile) : most_row_tiles(a, kAnyTile));
+    return with_half(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        hipLaunchKernelGGL((sk_experts_any<T, MODE>), dim3((unsigned)(parts_of(grid, 8) * 8)), dim3(kThreads), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+template <int MODE>
+hipError_t launch_product(const ExpertArgs &a, const Cut &c, hipStream_t st) {
+    if (c.tile == 256) return launch_tile<MODE, 256, 2, 4>(a, st);
+    if (c.tile == 128) return launch_tile<MODE, 128, 2, 2>(a, st);
+    return launch_tile<MODE, 64, 2, 2>(a, st);
+}
+
+hipError_t launch_rows_input(const ExpertArgs &a, hipStream_t st) {
+    return chunks(a) ? launch_product<kInput>(a, cut_rows(a, a.K), st) : launch_any<kInput>(a, st);
 }
 
 }  // namespace
 
 size_t experts_workspace_bytes(int T, int k, int K) { return (size_t)T * k * K * 4; }
 
+// Parts are taken where the sizes allow chunks; whether the pointers do shows in the call, which then needs none.
+size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
+    if (a.K % 8 || a.N % 8) return 0;
+    const Cut c = cut_weight(a);
+    return c.parts > 1 ? (size_t)c.parts * a.E * a.N * a.K * 4 : 0;
+}
+
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    return launch_product<kForward>(a, st);
+    if (!chunks(a)) return launch_any<kForward>(a, st);
+    // The weights are read once for each 16 rows of an expert.  256 rows, 64 experts of 2048 x 2048: 96 us, tiles 118;
+    // 512 rows, 64 of 1024 x 1024: 35 us, tiles 27.
+    const int64_t rows = (int64_t)a.T * a.k;
+    if (rows <= 64 || rows <= 4 * a.E) return launch_few(a, st);
+    return launch_product<kForward>(a, cut_rows(a, a.N), st);
 }
 
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    if (!a.slots) return launch_product<kInput>(a, st);
+    if (!a.slots) return launch_rows_input(a, st);
     ExpertArgs r = a;
     r.out32 = static_cast<float *>(ws);
-    const hipError_t e = launch_product<kInput>(r, st);
+    const hipError_t e = launch_rows_input(r, st);
     if (e != hipSuccess) return e;
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
@@ -571,8 +723,22 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
     });
 }
 
-hipError_t launch_experts_weight(const ExpertArgs &a, hipStream_t st) {
-    return launch_product<kWeight>(a, st);
+hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st) {
+    ExpertArgs r = a;
+    r.parts = 1;
+    if (!chunks(a) || !aligned16(ws)) return launch_any<kWeight>(r, st);
+    const Cut c = cut_weight(a);
+    r.parts = c.parts;
+    r.out32 = c.parts > 1 ? static_cast<float *>(ws) : nullptr;
+    const hipError_t e = launch_product<kWeight>(r, c, st);
+    if (e != hipSuccess || c.parts == 1) return e;
+    return with_half(a.dtype, [&](auto type) {
+        using T = decltype(type);
+        const int64_t n = (int64_t)a.E * a.N * a.K;
+        hipLaunchKernelGGL((sk_experts_sum_parts<T>), dim3((unsigned)parts_of(n, 8 * kThreads)), dim3(kThreads), 0, st,
+                           static_cast<const float *>(ws), static_cast<T *>(a.out), n, c.parts);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace sk

@@ -98,7 +98,8 @@ def _router(T, E, k, dtype, renormalize):
 @functools.lru_cache(maxsize=1024)
 def _experts(T, k, E, K, N, dtype):
     p = SkExperts(T, k, E, K, N, dtype)
-    return ctypes.byref(p), int(load_library().sinkhorn_experts_workspace_bytes(ctypes.byref(p)))
+    lib, ref = load_library(), ctypes.byref(p)
+    return ref, int(lib.sinkhorn_experts_workspace_bytes(ref)), int(lib.sinkhorn_experts_weight_workspace_bytes(ref))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -262,7 +263,7 @@ def sinkhorn_experts_forward(x, weight, offsets, tokens=None):
         _match(tokens, "tokens", x, None, torch.int32)
         rows = tokens.numel()
         k = _rows_of(rows, T, "tokens")
-    p, _ = _experts(T, k, E, K, N, _HALF[x.dtype])
+    p = _experts(T, k, E, K, N, _HALF[x.dtype])[0]
     y = torch.empty((rows, N), device=x.device, dtype=x.dtype)
     _call(load_library().sinkhorn_experts_forward, x.device, p, x.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
           _ptr(tokens), y.data_ptr())
@@ -275,14 +276,14 @@ def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspa
     E, N, K = _weight(weight)
     _half_rows(grad_y, "grad_y", N, weight)
     _match(offsets, "offsets", grad_y, (E + 1,), torch.int32)
-    T, k, need = grad_y.shape[0], 1, 0
+    T, k = grad_y.shape[0], 1
     if slots is not None:
         _match(slots, "slots", grad_y, None, torch.int32)
         if slots.dim() != 2 or slots.numel() != T:
             raise ValueError(f"slots must be [T, k] with T k = {T}, got {list(slots.shape)}")
         T = slots.shape[0]
         k = _rows_of(slots.numel(), T, "slots")
-    p, need = _experts(T, k, E, K, N, _HALF[grad_y.dtype])
+    p, need, _ = _experts(T, k, E, K, N, _HALF[grad_y.dtype])
     gx = torch.empty((T, K), device=grad_y.device, dtype=grad_y.dtype)
     scratch = None if slots is None else _scratch(workspace, need, grad_y.device)
     _call(load_library().sinkhorn_experts_backward_input, grad_y.device, p, grad_y.data_ptr(), weight.data_ptr(),
@@ -291,7 +292,7 @@ def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspa
 
 
 @_on_stream
-def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None):
+def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None, workspace=None):
     """Gradient of the weight, [E, N, K]."""
     _typed(grad_y, "grad_y", _HALF)
     if grad_y.dim() != 2 or x.dim() != 2:
@@ -306,10 +307,11 @@ def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None):
         k = _rows_of(rows, T, "tokens")
     elif T != rows:
         raise ValueError(f"without tokens x must have {rows} rows as grad_y, got {T}")
-    p, _ = _experts(T, k, E, K, N, _HALF[x.dtype])
+    p, _, need = _experts(T, k, E, K, N, _HALF[x.dtype])
     gw = torch.empty((E, N, K), device=x.device, dtype=x.dtype)
+    scratch = _scratch(workspace, need, x.device)
     _call(load_library().sinkhorn_experts_backward_weight, x.device, p, grad_y.data_ptr(), x.data_ptr(),
-          offsets.data_ptr(), _ptr(tokens), gw.data_ptr())
+          offsets.data_ptr(), _ptr(tokens), gw.data_ptr(), _ptr(scratch), need)
     return gw
 
 

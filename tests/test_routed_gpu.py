@@ -594,3 +594,16 @@ def test_refusals_of_gpu_tensors():
 def test_route_work_groups_of_many_threads(T, E, k):
     """Enough tokens for work-groups of 1024 threads, at each number of lanes to a token."""
     check_route(make_logits(T, E, BF16, T), k, mask=torch.rand(T, generator=gen(T)) < 0.9)
+
+
+@pytest.mark.parametrize("T,k,E,K,N", [(3000, 2, 2, 64, 72), (5000, 1, 1, 136, 80), (9000, 1, 3, 128, 128)])
+def test_products_weight_gradient_in_parts(T, k, E, K, N):
+    """Small matrices over many rows, one expert's share much larger than another's."""
+    check_products(T, k, E, K, N, BF16, seed=8, masked=True)
+
+
+def test_products_large_tiles():
+    """Enough rows and columns for the largest tiles, in each direction, with edges."""
+    check_products(4200, 2, 2, 264, 2056, BF16, seed=9, masked=True)
+    check_products(4200, 2, 2, 2056, 264, F16, seed=10)
+    check_products(600, 1, 33, 1032, 1000, BF16, seed=11)

@@ -56,8 +56,9 @@ def test_experts_refusals(args, code):
     p = b.SkExperts(*args)
     assert lib.sinkhorn_experts_forward(ctypes.byref(p), P, P, P, P, P, None) == code
     assert lib.sinkhorn_experts_backward_input(ctypes.byref(p), P, P, P, P, P, P, ctypes.c_size_t(0), None) == code
-    assert lib.sinkhorn_experts_backward_weight(ctypes.byref(p), P, P, P, P, P, None) == code
+    assert lib.sinkhorn_experts_backward_weight(ctypes.byref(p), P, P, P, P, P, P, ctypes.c_size_t(0), None) == code
     assert lib.sinkhorn_experts_workspace_bytes(ctypes.byref(p)) == 0
+    assert lib.sinkhorn_experts_weight_workspace_bytes(ctypes.byref(p)) == 0
 
 
 def test_experts_workspace_and_pointers():
@@ -71,7 +72,14 @@ def test_experts_workspace_and_pointers():
     assert back(ctypes.byref(p), P, P, P, P, None, P, ctypes.c_size_t(need), None) == -1
     assert lib.sinkhorn_experts_forward(ctypes.byref(p), None, P, P, P, P, None) == -1
     assert lib.sinkhorn_experts_forward(None, P, P, P, P, P, None) == -1
-    assert lib.sinkhorn_experts_backward_weight(ctypes.byref(p), P, None, P, P, P, None) == -1
+    weight = lib.sinkhorn_experts_backward_weight
+    assert weight(ctypes.byref(p), P, None, P, P, P, P, ctypes.c_size_t(1 << 30), None) == -1
+    many = b.SkExperts(16384, 2, 2, 128, 128, 1)  # two small matrices over many rows: summed in parts
+    need = lib.sinkhorn_experts_weight_workspace_bytes(ctypes.byref(many))
+    assert need >= 2 * 2 * 128 * 128 * 4 and need % (2 * 128 * 128 * 4) == 0
+    assert weight(ctypes.byref(many), P, P, P, P, P, P, ctypes.c_size_t(need - 1), None) == -5
+    assert weight(ctypes.byref(many), P, P, P, P, P, None, ctypes.c_size_t(need), None) == -1
+    assert lib.sinkhorn_experts_weight_workspace_bytes(ctypes.byref(b.SkExperts(64, 2, 8, 2048, 2048, 1))) == 0
     assert lib.sinkhorn_experts_forward(ctypes.byref(b.SkExperts(0, 2, 4, 64, 32, 1)), None, None, None, None, None,
                                         None) == 0
 
