@@ -289,11 +289,12 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         };
         // The step at d0 in `here`: FN products to a turn.  A turn reads the rows' fragment of two turns on and, towards
         // the end of the first half, a fragment of the second half's columns, and issues its share of the next step's
-        // copies (if there is one); the compiler may not move anything across turns, or it would read each fragment
-        // right before its use and wait for it.
+        // copies, if there is one: all in the first half, so that they land during the second (over all turns: 4 %
+        // slower).  The compiler may not move anything across turns, or it would read each fragment right before its
+        // use and wait for it.
         auto step = [&](auto next, auto partial, int d0, const char *here, char *there) {
-            constexpr int kTurns = kDeep / 32 * FM, kLead = 2, kEvery = kTurns / kCopies;
-            static_assert(kEvery * kCopies == kTurns && FM >= FN);
+            constexpr int kTurns = kDeep / 32 * FM, kLead = 2, kEach = kCopies / (kTurns / 2);
+            static_assert(kEach * (kTurns / 2) == kCopies && FM >= FN);
             all_copies();
             take_rows();
             look_up(d0 + 2 * kDeep);
@@ -310,10 +311,15 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                 const int j0 = i - (FM - FN);
                 if (j0 >= 0 && j0 < FN) fb[1][j0] = ob.frag(lb, j0, 1);
                 if constexpr (decltype(next)::value) {
-                    if (i % kEvery == 0) copy(partial, i / kEvery, d0 + kDeep, there);
+                    if (i < kTurns / 2) {
+#pragma unroll
+                        for (int c = i * kEach; c < (i + 1) * kEach; ++c) copy(partial, c, d0 + kDeep, there);
+                    }
                 }
+                __builtin_amdgcn_s_setprio(1);  // before the other wavefront's reads and copies
 #pragma unroll
                 for (int j = 0; j < FN; ++j) acc[i % FM][j] = mfma16<T>(fb[i / FM][j], fa[i], acc[i % FM][j]);
+                __builtin_amdgcn_s_setprio(0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             advance();
