@@ -146,7 +146,9 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     using OpB = Operand<T, MODE != kForward, BN, WAVES, FN>;
     constexpr int kStep = OpA::kBytes + OpB::kBytes;
     constexpr bool kWideA = WIDE && MODE == kForward, kWideB = WIDE && MODE == kWeight;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
+    constexpr int kOut = BM * (BN * 2 + 32);  // the results, below
+    static_assert(BM / WM * (BN * 4 + 32) <= kOut);
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kStep > kOut ? 2 * kStep : kOut];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int K = A.K, N = A.N, cols = MODE == kForward ? N : K;
@@ -340,26 +342,44 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         }
         step(no, no, d0, lds + odd * kStep, lds);
     }
-    // A lane holds four neighbouring columns of a row: row lane % 16, columns (lane / 16) * 4 of a 16 x 16 block.
+    // The results go through LDS, so that whole lines are written: a lane holds four neighbouring columns of a row (row
+    // lane % 16, columns (lane / 16) * 4 of a 16 x 16 block), 32 bytes a row of a block.  Written straight from there the
+    // products took 6 % longer.  Results in 32 bits go in WM passes, of BM / WM rows.
+    __syncthreads();  // nobody reads the last step's operands any more
+    const int64_t row0 = MODE == kWeight ? ((int64_t)part * A.E + e) * N : 0;
+    auto pass = [&](auto type, int rows0, int rows, bool mine) {
+        using O = decltype(type);
+        constexpr int kPitch = BN * (int)sizeof(O) + 32, kEach = 16 / (int)sizeof(O), kChunks = BN / kEach;
+        if (mine) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int row = m0 + wm + i * 16 + (lane & 15);
-        if (row >= m1) continue;
-        const int64_t base = (MODE == kWeight ? ((int64_t)part * A.E + e) * N + row : row) * (int64_t)cols;
+            for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int col = c0 + wn + j * 16 + (lane >> 4) * 4;
-            if (col >= cols) continue;
-            if (MODE != kForward && A.out32) {
-                *reinterpret_cast<f32x4 *>(A.out32 + base + col) = acc[i][j];
-            } else {
-                typedef T T4 __attribute__((ext_vector_type(4)));
-                T4 o;
+                for (int j = 0; j < FN; ++j) {
+                    typedef O O4 __attribute__((ext_vector_type(4)));
+                    O4 o;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[v] = (T)acc[i][j][v];
-                *reinterpret_cast<T4 *>(static_cast<T *>(A.out) + base + col) = o;
-            }
+                    for (int v = 0; v < 4; ++v) o[v] = (O)acc[i][j][v];
+                    *reinterpret_cast<O4 *>(lds + (wm - rows0 + i * 16 + (lane & 15)) * kPitch +
+                                            (wn + j * 16 + (lane >> 4) * 4) * (int)sizeof(O)) = o;
+                }
         }
+        __syncthreads();
+        for (int c = threadIdx.x; c < rows * kChunks; c += WAVES * 64) {
+            const int r = c / kChunks, row = m0 + rows0 + r, col = c0 + c % kChunks * kEach;
+            if (row >= m1 || col >= cols) continue;
+            const Words4 v = *reinterpret_cast<const Words4 *>(lds + r * kPitch + c % kChunks * 16);
+            char *out = sizeof(O) == 4 ? reinterpret_cast<char *>(A.out32) : static_cast<char *>(A.out);
+            *reinterpret_cast<Words4 *>(out + ((row0 + row) * cols + col) * (int)sizeof(O)) = v;
+        }
+    };
+    if (MODE != kForward && A.out32) {
+#pragma unroll
+        for (int q = 0; q < WM; ++q) {
+            if (q) __syncthreads();
+            pass(float{}, q * (BM / WM), BM / WM, wm == q * (BM / WM));
+        }
+    } else {
+        pass(T{}, 0, BM, true);
     }
 }
 
