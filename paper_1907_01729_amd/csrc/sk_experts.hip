@@ -138,8 +138,24 @@ struct Operand {
     }
 };
 
-// GATHERED: x's rows are looked up in tokens.  WIDE: x has 2^32 bytes or more.
-template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE>
+// `count` elements from p, at any alignment, zeros after them; count may be anything.
+template <class T>
+__device__ __forceinline__ Frag8<T> load_chunk(const T *p, int count) {
+    Frag8<T> v = {};
+    if (count >= 8) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < count) v[i] = p[i];
+    }
+    return v;
+}
+
+// GATHERED: x's rows are looked up in tokens.  WIDE: x has 2^32 bytes or more.  STAGED: rows that are no whole chunks of
+// 16 bytes, or pointers that are not aligned to them: the chunks come through registers, loaded at the start of a step
+// and written to LDS at its end.
+template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE, bool STAGED>
 __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void sk_experts_tile(ExpertArgs A) {
     constexpr int WAVES = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
     using OpA = Operand<T, MODE == kWeight, BM, WAVES, FM>;
@@ -218,7 +234,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             for (int q = 0; q < OpA::kRounds; ++q) {
                 const int r = OpA::copy_row(q, wave, lane), c = OpA::copy_element(q, wave, lane);
                 from_a[q] = MODE == kInput ? (uint32_t)(min(r, m1 - 1 - m0) * N + c) * 2
-                                           : (uint32_t)(r * N + min(c, N - 8 - m0)) * 2;
+                                           : (uint32_t)(r * N + (STAGED ? c : min(c, N - 8 - m0))) * 2;
             }
         }
         if constexpr (MODE == kWeight) {
@@ -231,7 +247,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             const int r = OpB::copy_row(q, wave, lane), c = OpB::copy_element(q, wave, lane);
             if constexpr (!kLookUp)
                 from_b[q] = MODE == kForward ? (uint32_t)(min(r, N - 1 - c0) * K + c) * 2
-                                             : (uint32_t)(r * K + min(c, K - 8 - c0)) * 2;
+                                             : (uint32_t)(r * K + (STAGED ? c : min(c, K - 8 - c0))) * 2;
         }
         auto look_up = [&](int d0) {
             if constexpr (kLookUp) {
@@ -247,7 +263,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                     // To the compiler, a wait for the look-up: here, where no copy is under way.
                     asm volatile("" : "+v"(token[q]));
                     const int t = token[q] >= 0 && token[q] < A.T ? token[q] : 0;
-                    const int c = min(OpB::copy_element(q, wave, lane), K - 8 - c0);
+                    const int e8 = OpB::copy_element(q, wave, lane), c = STAGED ? e8 : min(e8, K - 8 - c0);
                     if constexpr (kWideB)
                         from_b[q] = base_b + ((int64_t)t * K + c) * 2;
                     else
@@ -257,11 +273,33 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         };
         // Copy c of the step at d0.  PARTIAL: the contraction ends within the step, zeros from there.
         constexpr int kCopies = OpA::kRounds + OpB::kRounds;
+        Frag8<T> held[STAGED ? kCopies : 1];
+        auto place = [&](int c) {
+            return c < OpA::kRounds ? (c * WAVES + wave) * 1024
+                                    : OpA::kBytes + ((c - OpA::kRounds) * WAVES + wave) * 1024;
+        };
         auto copy = [&](auto partial, int c, int d0, char *to) {
             const bool is_a = c < OpA::kRounds;
             const int q = is_a ? c : c - OpA::kRounds;
-            to += (is_a ? 0 : OpA::kBytes) + (q * WAVES + wave) * 1024;
-            if constexpr (decltype(partial)::value) {
+            to += place(c);
+            if constexpr (STAGED) {
+                // How many of the chunk's elements there are, along the contraction or across the tile.
+                const int left = deep - d0;
+                const char *from;
+                int count;
+                if (is_a) {
+                    const int r = OpA::copy_row(q, wave, lane), el = OpA::copy_element(q, wave, lane);
+                    count = MODE != kWeight ? left - el : r < left ? N - m0 - el : 0;
+                    if constexpr (kWideA) from = from_a[q];
+                    else from = base_a + from_a[q];
+                } else {
+                    const int r = OpB::copy_row(q, wave, lane), el = OpB::copy_element(q, wave, lane);
+                    count = MODE == kForward ? left - el : r < left ? K - c0 - el : 0;
+                    if constexpr (kWideB) from = from_b[q];
+                    else from = base_b + from_b[q];
+                }
+                held[c] = load_chunk(reinterpret_cast<const T *>(from), count);
+            } else if constexpr (decltype(partial)::value) {
                 const char *from;
                 if (is_a) {
                     if constexpr (kWideA) from = from_a[q];
@@ -277,6 +315,13 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                 copy16<kWideA>(base_a, from_a[q], to);
             } else {
                 copy16<kWideB>(base_b, from_b[q], to);
+            }
+        };
+        // STAGED: the chunks of the step's copies, to their places in LDS.
+        auto put = [&](char *to) {
+            if constexpr (STAGED) {
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c) *reinterpret_cast<Frag8<T> *>(to + place(c) + lane * 16) = held[c];
             }
         };
         // On to the next step's places.
@@ -324,6 +369,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                 __builtin_amdgcn_s_setprio(0);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (decltype(next)::value) put(there);
             advance();
         };
         constexpr std::true_type yes{};
@@ -332,6 +378,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         take_rows();
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) copy(yes, c, 0, lds);
+        put(lds);
         advance();
         look_up(kDeep);
         int d0 = 0, odd = 0;
@@ -369,7 +416,15 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             if (row >= m1 || col >= cols) continue;
             const Words4 v = *reinterpret_cast<const Words4 *>(lds + r * kPitch + c % kChunks * 16);
             char *out = sizeof(O) == 4 ? reinterpret_cast<char *>(A.out32) : static_cast<char *>(A.out);
-            *reinterpret_cast<Words4 *>(out + ((row0 + row) * cols + col) * (int)sizeof(O)) = v;
+            out += ((row0 + row) * cols + col) * (int)sizeof(O);
+            if constexpr (!STAGED) {
+                *reinterpret_cast<Words4 *>(out) = v;
+            } else if (cols - col >= kEach) {
+                __builtin_memcpy(out, &v, 16);
+            } else {
+                for (int i = 0; i < cols - col; ++i)
+                    reinterpret_cast<O *>(out)[i] = reinterpret_cast<const O *>(lds + r * kPitch + c % kChunks * 16)[i];
+            }
         }
     };
     if (MODE != kForward && A.out32) {
@@ -449,109 +504,6 @@ __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     const T2 out = {(T)sum[0], (T)sum[1]};
     *reinterpret_cast<T2 *>(static_cast<T *>(A.out) + (int64_t)(t.begin + r) * N + c0 + c) = out;
-}
-
-// ---- any sizes and alignment: 64 x 64 tiles, elements loaded one by one ----
-
-constexpr int kAnyTile = 64, kAnyDeep = 32, kAnyPitch = kAnyDeep + 8;
-
-template <class T, int MODE>
-__global__ __launch_bounds__(kThreads) void sk_experts_any(ExpertArgs A) {
-    __shared__ T la[kAnyTile * kAnyPitch], lb[kAnyTile * kAnyPitch];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T *x = static_cast<const T *>(A.x), *w = static_cast<const T *>(A.w), *gy = static_cast<const T *>(A.gy);
-    const int K = A.K, N = A.N;
-
-    int e, r0, r1, c0, m0 = 0;  // the expert, its rows here, the first column; weight: the first row of gw's tile
-    if constexpr (MODE == kWeight) {
-        const int tk = (K + kAnyTile - 1) / kAnyTile, tn = (N + kAnyTile - 1) / kAnyTile;
-        const int t = xcd_order(blockIdx.x, A.E * tk * tn);
-        if (t < 0) return;
-        e = t / (tk * tn);
-        const int rest = t - e * (tk * tn);
-        m0 = rest / tk * kAnyTile;
-        c0 = rest % tk * kAnyTile;
-        const RowRange rr = expert_rows(A, e);
-        r0 = rr.begin, r1 = rr.end;
-    } else {
-        const int cols = MODE == kForward ? N : K;
-        const Tile t = find_tile(A, kAnyTile, (cols + kAnyTile - 1) / kAnyTile, blockIdx.x);
-        if (t.expert < 0) return;
-        e = t.expert, r0 = t.begin, r1 = t.end;
-        c0 = t.column * kAnyTile;
-    }
-    const T *we = w + (size_t)(e < A.E ? e : 0) * N * K;
-    const int deep = MODE == kForward ? K : MODE == kInput ? N : r1 - r0;
-    const bool none = MODE != kWeight && e >= A.E;  // rows of no expert: zeros
-
-    auto source = [&](int r) -> int64_t {  // x's row of a row, -1: none
-        if (!A.tokens) return r;
-        const int t = A.tokens[r];
-        return t >= 0 && t < A.T ? t : -1;
-    };
-    auto load_a = [&](int i, int d) -> T {  // row i of the tile, d of the contraction
-        if (d >= deep) return (T)0.f;
-        if constexpr (MODE == kWeight) {
-            return m0 + i < N ? gy[(int64_t)(r0 + d) * N + m0 + i] : (T)0.f;
-        } else {
-            if (r0 + i >= r1) return (T)0.f;
-            if constexpr (MODE == kInput) return gy[(int64_t)(r0 + i) * N + d];
-            const int64_t s = source(r0 + i);
-            return s >= 0 ? x[s * K + d] : (T)0.f;
-        }
-    };
-    auto load_b = [&](int j, int d) -> T {  // column j of the tile
-        if (d >= deep) return (T)0.f;
-        if constexpr (MODE == kForward) return c0 + j < N ? we[(int64_t)(c0 + j) * K + d] : (T)0.f;
-        if constexpr (MODE == kInput) return c0 + j < K ? we[(int64_t)d * K + c0 + j] : (T)0.f;
-        const int64_t s = source(r0 + d);
-        return c0 + j < K && s >= 0 ? x[s * K + c0 + j] : (T)0.f;
-    };
-
-    f32x4 acc[2][2] = {};
-    const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-    for (int d0 = 0; !none && d0 < deep; d0 += kAnyDeep) {
-        __syncthreads();
-        for (int q = tid; q < kAnyTile * kAnyDeep; q += kThreads) {
-            // neighbours in memory to neighbouring lanes
-            const int i = MODE == kWeight ? q % kAnyTile : q / kAnyDeep, d = MODE == kWeight ? q / kAnyTile : q % kAnyDeep;
-            la[i * kAnyPitch + d] = load_a(i, d0 + d);
-            const int j = MODE == kForward ? q / kAnyDeep : q % kAnyTile, f = MODE == kForward ? q % kAnyDeep : q / kAnyTile;
-            lb[j * kAnyPitch + f] = load_b(j, d0 + f);
-        }
-        __syncthreads();
-        Frag8<T> fa[2], fb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fa[i] = *reinterpret_cast<const Frag8<T> *>(la + (wi + i * 16 + (lane & 15)) * kAnyPitch + (lane >> 4) * 8);
-            fb[i] = *reinterpret_cast<const Frag8<T> *>(lb + (wj + i * 16 + (lane & 15)) * kAnyPitch + (lane >> 4) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mfma16<T>(fa[i], fb[j], acc[i][j]);
-    }
-    // lane: column lane % 16, rows (lane / 16) * 4 + v of a 16 x 16 block
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int row = wi + i * 16 + (lane >> 4) * 4 + v, col = c0 + wj + j * 16 + (lane & 15);
-                if constexpr (MODE == kWeight) {
-                    if (m0 + row < N && col < K)
-                        static_cast<T *>(A.out)[((size_t)e * N + m0 + row) * K + col] = (T)acc[i][j][v];
-                } else {
-                    const int cols = MODE == kForward ? N : K;
-                    if (r0 + row >= r1 || col >= cols) continue;
-                    const int64_t at = (int64_t)(r0 + row) * cols + col;
-                    if (A.out32)
-                        A.out32[at] = acc[i][j][v];
-                    else
-                        static_cast<T *>(A.out)[at] = (T)acc[i][j][v];
-                }
-            }
 }
 
 // gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here.  Eight elements of gx to a
@@ -654,7 +606,7 @@ bool chunks(const ExpertArgs &a) {
            (!a.gy || aligned16(a.gy)) && aligned16(a.out) && aligned16(a.out32);
 }
 
-template <int MODE, int TILE, int WM, int WN>
+template <int MODE, int TILE, int WM, int WN, bool STAGED = false>
 hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
     const int64_t tiles = MODE == kWeight ? a.E * parts_of(a.N, TILE) * parts_of(a.K, TILE) * a.parts
                                           : most_row_tiles(a, TILE) * parts_of(MODE == kForward ? a.N : a.K, TILE);
@@ -664,12 +616,17 @@ hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(parts_of(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
             return hipGetLastError();
         };
-        if constexpr (MODE != kInput) {
-            if (a.tokens && (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32))
-                return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, true, true>);
-            if (a.tokens) return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, true, false>);
+        constexpr bool kGathers = MODE != kInput;
+        if constexpr (STAGED) {
+            if (a.tokens && kGathers) return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, kGathers, true>);
+            return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false, true>);
+        } else {
+            if (a.tokens && kGathers)
+                return (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32)
+                           ? go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, kGathers, false>)
+                           : go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, false, false>);
+            return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false, false>);
         }
-        return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false>);
     });
 }
 
@@ -687,25 +644,16 @@ hipError_t launch_few(const ExpertArgs &a, hipStream_t st) {
 }
 
 template <int MODE>
-hipError_t launch_any(const ExpertArgs &a, hipStream_t st) {
-    const int64_t cols = parts_of(MODE == kForward ? a.N : a.K, kAnyTile);
-    const int64_t grid = cols * (MODE == kWeight ? a.E * parts_of(a.N, kAnyTile) : most_row_tiles(a, kAnyTile));
-    return with_half(a.dtype, [&](auto type) {
-        using T = decltype(type);
-        hipLaunchKernelGGL((sk_experts_any<T, MODE>), dim3((unsigned)(parts_of(grid, 8) * 8)), dim3(kThreads), 0, st, a);
-        return hipGetLastError();
-    });
-}
-
-template <int MODE>
 hipError_t launch_product(const ExpertArgs &a, const Cut &c, hipStream_t st) {
+    if (!chunks(a))
+        return c.tile == 64 ? launch_tile<MODE, 64, 2, 2, true>(a, st) : launch_tile<MODE, 128, 2, 2, true>(a, st);
     if (c.tile == 256) return launch_tile<MODE, 256, 2, 4>(a, st);
     if (c.tile == 128) return launch_tile<MODE, 128, 2, 2>(a, st);
     return launch_tile<MODE, 64, 2, 2>(a, st);
 }
 
 hipError_t launch_rows_input(const ExpertArgs &a, hipStream_t st) {
-    return chunks(a) ? launch_product<kInput>(a, cut_rows(a, a.K), st) : launch_any<kInput>(a, st);
+    return launch_product<kInput>(a, cut_rows(a, a.K), st);
 }
 
 }  // namespace
@@ -721,11 +669,10 @@ size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
 
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    if (!chunks(a)) return launch_any<kForward>(a, st);
     // The weights are read once for each 16 rows of an expert.  256 rows, 64 experts of 2048 x 2048: 96 us, tiles 118;
     // 512 rows, 64 of 1024 x 1024: 35 us, tiles 27.
     const int64_t rows = (int64_t)a.T * a.k;
-    if (rows <= 64 || rows <= 4 * a.E) return launch_few(a, st);
+    if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, a.N), st);
 }
 
@@ -752,8 +699,8 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
 hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st) {
     ExpertArgs r = a;
     r.parts = 1;
-    if (!chunks(a) || !aligned16(ws)) return launch_any<kWeight>(r, st);
-    const Cut c = cut_weight(a);
+    Cut c = cut_weight(a);
+    if (!chunks(a) || !aligned16(ws)) c.parts = 1;
     r.parts = c.parts;
     r.out32 = c.parts > 1 ? static_cast<float *>(ws) : nullptr;
     const hipError_t e = launch_product<kWeight>(r, c, st);

@@ -607,3 +607,8 @@ def test_products_large_tiles():
     check_products(4200, 2, 2, 264, 2056, BF16, seed=9, masked=True)
     check_products(4200, 2, 2, 2056, 264, F16, seed=10)
     check_products(600, 1, 33, 1032, 1000, BF16, seed=11)
+
+
+def test_products_odd_sizes_large_tiles():
+    check_products(3000, 2, 3, 1033, 1031, BF16, seed=12, masked=True)
+    check_products(2500, 1, 2, 262, 1027, F16, seed=13, gathered=False)
