@@ -202,6 +202,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 
     f32x4 acc[FM][FN] = {};
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    const bool idle = m0 + wm >= m1 || c0 + wn >= cols;  // the wavefront's part lies past the edge: it copies only
     if (deep > 0) {
         OpA oa;
         OpB ob;
@@ -381,13 +382,30 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         put(lds);
         advance();
         look_up(kDeep);
-        int d0 = 0, odd = 0;
-        for (; d0 + 2 * kDeep <= deep; d0 += kDeep, odd ^= 1) step(yes, no, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
-        if (d0 + kDeep < deep) {
-            step(yes, yes, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
-            d0 += kDeep, odd ^= 1;
-        }
-        step(no, no, d0, lds + odd * kStep, lds);
+        auto run = [&](auto one_step) {
+            int d0 = 0, odd = 0;
+            for (; d0 + 2 * kDeep <= deep; d0 += kDeep, odd ^= 1)
+                one_step(yes, no, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
+            if (d0 + kDeep < deep) {
+                one_step(yes, yes, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
+                d0 += kDeep, odd ^= 1;
+            }
+            one_step(no, no, d0, lds + odd * kStep, lds);
+        };
+        if (idle)
+            run([&](auto next, auto partial, int d0, const char *, char *there) {
+                all_copies();
+                take_rows();
+                look_up(d0 + 2 * kDeep);
+                if constexpr (decltype(next)::value) {
+#pragma unroll
+                    for (int c = 0; c < kCopies; ++c) copy(partial, c, d0 + kDeep, there);
+                    put(there);
+                }
+                advance();
+            });
+        else
+            run(step);
     }
     // The results go through LDS, so that whole lines are written: a lane holds four neighbouring columns of a row (row
     // lane % 16, columns (lane / 16) * 4 of a 16 x 16 block), 32 bytes a row of a block.  Written straight from there the
