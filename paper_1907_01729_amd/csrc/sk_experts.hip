@@ -592,9 +592,9 @@ struct Cut {
 // Rows' products.  The expected number of tiles (half a tile of each expert is empty) decides.  256: one work-group a
 // CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each other's first
 // copies and last writes.  64: too few tiles of 128 to go round.  Measured, 256 / 128 / 64, in us: 65536 rows of 64
-// experts of 2048 x 2048 (9.0 rounds) 600 / 620 / -; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 169 / 157 / 217; 8000
-// rows of 2 of 2048 x 1024 (1.0) 39 / 45 / 64; 2331 rows of 12 of 520 x 1000 25 / 12.5 / 11.3; 300 rows of 2 of
-// 2048 x 2048 43 / 18.5 / 12.4.
+// experts of 2048 x 2048 (9.0 rounds) 527 / 609 / 914; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 147 / 143 / 205; 8000
+// rows of 2 of 2048 x 1024 (1.0) 34 / 39 / 62; 2331 rows of 12 of 520 x 1000 25 / 12.5 / 11.6; 300 rows of 2 of
+// 2048 x 2048 40 / 17 / 12.
 Cut cut_rows(const ExpertArgs &a, int cols) {
     const int64_t rows = (int64_t)a.T * a.k;
     auto tiles = [&](int64_t tile) { return (rows / tile + (a.E + 1) / 2) * parts_of(cols, tile); };
@@ -604,18 +604,21 @@ Cut cut_rows(const ExpertArgs &a, int cols) {
 }
 
 // Weight gradients.  256 where there are two rounds of it and its edges waste no more than 128's would; else 128, or 64
-// for narrow matrices.  Few tiles over many rows are cut along the rows, into parts of eight steps or more, until there
-// are two work-groups a CU.  Measured, whole / in parts: 65536 rows of 16 experts of 512 x 512 118 / 76 us, 32768 rows
-// of 2 of 128 x 128 198 / 20.5 us; 256 / 128: 8192 rows of 8 of 4096 x 2048 221 / 248 us, 10308 rows of 28 of 272 x 1592
-// 46 / 41 us.
+// where that makes too few work-groups.  Few tiles over many rows are cut along the rows, into parts of eight steps or
+// more, until there are two work-groups a CU.  Measured, in us: 256 / 128: 8192 rows of 8 of 4096 x 2048 197 / 231,
+// 24000 rows of 32 of 2048 x 1024 147 / 174; 128 / 64: 9620 rows of 14 of 96 x 80 16.4 / 10.9; whole / in parts: 65536
+// rows of 16 experts of 512 x 512 111 / 73, 32768 rows of 2 of 128 x 128 131 / 19.
 Cut cut_weight(const ExpertArgs &a) {
     auto tiles = [&](int64_t tile) { return a.E * parts_of(a.N, tile) * parts_of(a.K, tile); };
     if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1};
-    const int tile = a.N <= 64 || a.K <= 64 ? 64 : 128;
-    const int64_t n = tiles(tile), steps = parts_of((int64_t)a.T * a.k, (int64_t)a.E * kDeep);
-    int64_t parts = parts_of(512, n);
-    if (parts > steps / 8) parts = steps / 8;
-    return {tile, (int)(parts < 1 ? 1 : parts)};
+    const int64_t steps = parts_of((int64_t)a.T * a.k, (int64_t)a.E * kDeep);
+    auto cut = [&](int tile) {
+        int64_t parts = parts_of(512, tiles(tile));
+        if (parts > steps / 8) parts = steps / 8;
+        return Cut{tile, (int)(parts < 1 ? 1 : parts)};
+    };
+    const Cut c = cut(128);
+    return tiles(128) * c.parts >= 256 ? c : cut(64);
 }
 
 // Whether rows can be copied in chunks of 16 bytes.
@@ -687,8 +690,8 @@ size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
 
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    // The weights are read once for each 16 rows of an expert.  256 rows, 64 experts of 2048 x 2048: 96 us, tiles 118;
-    // 512 rows, 64 of 1024 x 1024: 35 us, tiles 27.
+    // The weights are read once for each 16 rows of an expert.  256 rows, 64 experts of 2048 x 2048: 95 us, tiles 115;
+    // 512 rows, 64 of 1024 x 1024: 34 us, tiles 28.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, a.N), st);

@@ -17,6 +17,7 @@ import functools
 from typing import NamedTuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, load_library
 
@@ -203,6 +204,7 @@ class _Route(torch.autograd.Function):
         return tuple(r)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_weights, _e, _c, _o, _t, _s, g_balance, g_z):
         logits, weights, experts, counts, state = ctx.saved_tensors
         return _route_backward(logits, ctx.k, weights, experts, counts, state, _contiguous(g_weights),
@@ -322,6 +324,7 @@ class _ExpertProduct(torch.autograd.Function):
         return sinkhorn_experts_forward(x, weight, offsets, tokens)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, weight, offsets, tokens, slots = ctx.saved_tensors
         gy = gy.contiguous()
@@ -362,6 +365,7 @@ class _Dropout(torch.autograd.Function):
         return _run_dropout(x, residual, counter)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         gx = _run_dropout(gy.contiguous(), None, ctx.counter) if ctx.needs_input_grad[0] else None
         return gx, gy if ctx.needs_input_grad[1] else None, None
@@ -445,6 +449,7 @@ class _Combine(torch.autograd.Function):
         return _run_combine(z, weights, slots, residual, *sizes, counter)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         z, weights, slots, offsets = ctx.saved_tensors
         gz = gw = None

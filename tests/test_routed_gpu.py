@@ -612,3 +612,58 @@ def test_products_large_tiles():
 def test_products_odd_sizes_large_tiles():
     check_products(3000, 2, 3, 1033, 1031, BF16, seed=12, masked=True)
     check_products(2500, 1, 2, 262, 1027, F16, seed=13, gathered=False)
+
+
+@pytest.mark.parametrize("T", [800_000, 1_200_000])
+def test_products_of_long_inputs(T):
+    """Inputs past 2^31 and past 2^32 bytes: rows near the end, forward and weight gradient."""
+    K, N, E = 2048, 64, 4
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, K, generator=g, device="cuda", dtype=BF16)
+    w = (torch.randn(E, N, K, generator=g, device="cuda") / math.sqrt(K)).to(BF16)
+    experts = torch.randint(0, E, (T, 1), generator=g, device="cuda").int().cpu()
+    offsets, tokens, slots = (t.cuda() for t in ref.order_of(experts, E))
+    y = sk.sinkhorn_experts_forward(x, w, offsets, tokens)
+    some = torch.cat([torch.arange(0, 300), torch.arange(T // 2, T // 2 + 300), torch.arange(T - 300, T)]).cuda()
+    rows = slots[some, 0].long()
+    mine = experts.cuda()[some, 0].long()
+    xs = x[some].double()
+    want = torch.stack([torch.mv(w[e].double(), v) for e, v in zip(mine.tolist(), xs)])
+    size = torch.stack([torch.mv(w[e].double().abs(), v.abs()) for e, v in zip(mine.tolist(), xs)])
+    within(y[rows], want.cpu(), rounding(want.cpu(), BF16) + 2 * (K + 8) * E32 * size.cpu())
+    gy = torch.zeros(T, N, device="cuda", dtype=BF16)
+    gs = torch.randn(len(some), N, generator=g, device="cuda").to(BF16)
+    gy[rows] = gs
+    gw = sk.sinkhorn_experts_backward_weight(gy, x, offsets, tokens)
+    want, size = torch.zeros(E, N, K, dtype=torch.float64), torch.zeros(E, N, K, dtype=torch.float64)
+    for e in range(E):
+        at = (mine == e).nonzero()[:, 0]
+        want[e] = (gs[at].double().t().contiguous() @ xs[at]).cpu()
+        size[e] = (gs[at].double().abs().t().contiguous() @ xs[at].abs()).cpu()
+    # the other rows' products are zeros: they add nothing
+    within(gw, want, rounding(want, BF16) + 2 * (len(some) + 8) * E32 * size)
+
+
+def test_one_gradient_alone():
+    args = layer_inputs(90, 6)
+    x, w = args[0], args[2]
+    r = sk.sinkhorn_route(args[1], 2)
+    gy = torch.ones(180, 96, device="cuda", dtype=BF16)
+    both = torch.autograd.grad(sk.sinkhorn_expert_product(x.requires_grad_(), w.requires_grad_(), r.offsets, r.tokens,
+                                                          r.slots), (x, w), gy)
+    gx, = torch.autograd.grad(sk.sinkhorn_expert_product(x, w.detach(), r.offsets, r.tokens, r.slots), (x,), gy)
+    gw, = torch.autograd.grad(sk.sinkhorn_expert_product(x.detach(), w, r.offsets, r.tokens, r.slots), (w,), gy)
+    assert torch.equal(gx, both[0]) and torch.equal(gw, both[1])
+    z = torch.randn(180, 64, device="cuda")
+    weights = r.weights.clone().requires_grad_()
+    y = sk.sinkhorn_expert_combine(z, weights, r.slots, r.offsets, p=0.2, seed=3)
+    g, = torch.autograd.grad(y.sum(), (weights,))
+    _, want = sk.sinkhorn_combine_backward(z, weights.detach(), r.slots, r.offsets, torch.ones_like(y), 0.2, 3)
+    assert torch.equal(g, want)
+
+
+def test_no_second_derivative():
+    x = torch.randn(8, device="cuda", requires_grad=True)
+    g, = torch.autograd.grad((sk.sinkhorn_dropout(x, 0.1, 1) * x).sum(), (x,), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
