@@ -78,6 +78,17 @@ def _call(fn, dev, *args):
         raise SinkhornError(status, fn.__name__)
 
 
+def _first_order(fn):
+    """A backward pass that has no derivative itself: who asks for one gets an error.  Only where a graph is built for
+    it, since the wrapper takes ten microseconds of a backward pass."""
+    refuses = once_differentiable(fn)
+
+    @functools.wraps(fn)
+    def backward(ctx, *grads):
+        return refuses(ctx, *grads) if torch.is_grad_enabled() else fn(ctx, *grads)
+    return backward
+
+
 def _on_stream(fn):
     """Gives fn a keyword argument stream: the call, its outputs and its workspace on that stream."""
     @functools.wraps(fn)
@@ -204,7 +215,7 @@ class _Route(torch.autograd.Function):
         return tuple(r)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, g_weights, _e, _c, _o, _t, _s, g_balance, g_z):
         logits, weights, experts, counts, state = ctx.saved_tensors
         return _route_backward(logits, ctx.k, weights, experts, counts, state, _contiguous(g_weights),
@@ -256,19 +267,25 @@ def _weight(w):
 def sinkhorn_experts_forward(x, weight, offsets, tokens=None):
     """Rows of each expert times its matrix: y [R, N].  x [T, K] gathered through tokens [R], or, without tokens,
     x [R, K] in the rows' order; weight [E, N, K]; offsets [E + 1]."""
+    return _run_experts(x, weight, offsets, tokens, _experts_sizes(x, weight, offsets, tokens))
+
+
+def _experts_sizes(x, weight, offsets, tokens):
     E, N, K = _weight(weight)
     _half_rows(x, "x", K, weight)
     _match(offsets, "offsets", x, (E + 1,), torch.int32)
-    rows = T = x.shape[0]
-    k = 1
+    T, k = x.shape[0], 1
     if tokens is not None:
         _match(tokens, "tokens", x, None, torch.int32)
-        rows = tokens.numel()
-        k = _rows_of(rows, T, "tokens")
-    p = _experts(T, k, E, K, N, _HALF[x.dtype])[0]
-    y = torch.empty((rows, N), device=x.device, dtype=x.dtype)
-    _call(load_library().sinkhorn_experts_forward, x.device, p, x.data_ptr(), weight.data_ptr(), offsets.data_ptr(),
-          _ptr(tokens), y.data_ptr())
+        k = _rows_of(tokens.numel(), T, "tokens")
+    return T, k, E, K, N, _HALF[x.dtype]
+
+
+def _run_experts(x, weight, offsets, tokens, sizes):
+    T, k, _, _, N, _ = sizes
+    y = torch.empty((T * k, N), device=x.device, dtype=x.dtype)
+    _call(load_library().sinkhorn_experts_forward, x.device, _experts(*sizes)[0], x.data_ptr(), weight.data_ptr(),
+          offsets.data_ptr(), _ptr(tokens), y.data_ptr())
     return y
 
 
@@ -285,8 +302,12 @@ def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspa
             raise ValueError(f"slots must be [T, k] with T k = {T}, got {list(slots.shape)}")
         T = slots.shape[0]
         k = _rows_of(slots.numel(), T, "slots")
-    p, need, _ = _experts(T, k, E, K, N, _HALF[grad_y.dtype])
-    gx = torch.empty((T, K), device=grad_y.device, dtype=grad_y.dtype)
+    return _run_experts_input(grad_y, weight, offsets, slots, (T, k, E, K, N, _HALF[grad_y.dtype]), workspace)
+
+
+def _run_experts_input(grad_y, weight, offsets, slots, sizes, workspace=None):
+    p, need, _ = _experts(*sizes)
+    gx = torch.empty((sizes[0], sizes[3]), device=grad_y.device, dtype=grad_y.dtype)
     scratch = None if slots is None else _scratch(workspace, need, grad_y.device)
     _call(load_library().sinkhorn_experts_backward_input, grad_y.device, p, grad_y.data_ptr(), weight.data_ptr(),
           offsets.data_ptr(), _ptr(slots), gx.data_ptr(), _ptr(scratch), need)
@@ -309,7 +330,12 @@ def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None, workspace=
         k = _rows_of(rows, T, "tokens")
     elif T != rows:
         raise ValueError(f"without tokens x must have {rows} rows as grad_y, got {T}")
-    p, _, need = _experts(T, k, E, K, N, _HALF[x.dtype])
+    return _run_experts_weight(grad_y, x, offsets, tokens, (T, k, E, K, N, _HALF[x.dtype]), workspace)
+
+
+def _run_experts_weight(grad_y, x, offsets, tokens, sizes, workspace=None):
+    _, _, E, K, N, _ = sizes
+    p, _, need = _experts(*sizes)
     gw = torch.empty((E, N, K), device=x.device, dtype=x.dtype)
     scratch = _scratch(workspace, need, x.device)
     _call(load_library().sinkhorn_experts_backward_weight, x.device, p, grad_y.data_ptr(), x.data_ptr(),
@@ -319,18 +345,19 @@ def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None, workspace=
 
 class _ExpertProduct(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, offsets, tokens, slots):
+    def forward(ctx, x, weight, offsets, tokens, slots, sizes):
         ctx.save_for_backward(x, weight, offsets, tokens, slots)
-        return sinkhorn_experts_forward(x, weight, offsets, tokens)
+        ctx.sizes = sizes
+        return _run_experts(x, weight, offsets, tokens, sizes)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, gy):
         x, weight, offsets, tokens, slots = ctx.saved_tensors
-        gy = gy.contiguous()
-        gx = sinkhorn_experts_backward_input(gy, weight, offsets, slots) if ctx.needs_input_grad[0] else None
-        gw = sinkhorn_experts_backward_weight(gy, x, offsets, tokens) if ctx.needs_input_grad[1] else None
-        return gx, gw, None, None, None
+        gy, need_x, need_w = gy.contiguous(), *ctx.needs_input_grad[:2]
+        gx = _run_experts_input(gy, weight, offsets, slots, ctx.sizes) if need_x else None
+        gw = _run_experts_weight(gy, x, offsets, tokens, ctx.sizes) if need_w else None
+        return gx, gw, None, None, None, None
 
 
 def sinkhorn_expert_product(x, weight, offsets, tokens=None, slots=None):
@@ -341,12 +368,13 @@ def sinkhorn_expert_product(x, weight, offsets, tokens=None, slots=None):
     if (tokens is None) != (slots is None):
         raise ValueError("tokens and slots go together")
     x, weight = x.contiguous(), weight.contiguous()
-    if slots is not None and (slots.dim() != 2 or slots.shape[0] != x.shape[0] or slots.numel() != tokens.numel()):
-        raise ValueError(f"slots must be [T, k] with T = {x.shape[0]}, T k = {tokens.numel()}, "
-                         f"got {list(slots.shape)}")
+    sizes = _experts_sizes(x, weight, offsets, tokens)
+    if slots is not None:
+        T, k = sizes[:2]
+        _match(slots, "slots", x, (T, k) if T else (0, *slots.shape[1:2]), torch.int32)
     if (x.requires_grad or weight.requires_grad) and torch.is_grad_enabled():
-        return _ExpertProduct.apply(x, weight, offsets, tokens, slots)
-    return sinkhorn_experts_forward(x, weight, offsets, tokens)
+        return _ExpertProduct.apply(x, weight, offsets, tokens, slots, sizes)
+    return _run_experts(x, weight, offsets, tokens, sizes)
 
 
 # ---- dropout ----
@@ -365,7 +393,7 @@ class _Dropout(torch.autograd.Function):
         return _run_dropout(x, residual, counter)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, gy):
         gx = _run_dropout(gy.contiguous(), None, ctx.counter) if ctx.needs_input_grad[0] else None
         return gx, gy if ctx.needs_input_grad[1] else None, None
@@ -449,7 +477,7 @@ class _Combine(torch.autograd.Function):
         return _run_combine(z, weights, slots, residual, *sizes, counter)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, gy):
         z, weights, slots, offsets = ctx.saved_tensors
         gz = gw = None
