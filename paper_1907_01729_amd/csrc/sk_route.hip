@@ -25,6 +25,9 @@ constexpr int kBlocksWanted = 512;
 constexpr int kManyThreads = 1024;
 constexpr uint32_t kNoPair = 0xFFFFFFFFu;
 
+// v_rcp_f32, to one unit in the last place: a full division is ten instructions.
+__device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
+
 // Reductions over aligned groups of L lanes; every lane of the group ends with the same bits.
 template <int L>
 __device__ __forceinline__ float group_sum(float v) {
@@ -244,7 +247,7 @@ __global__ __launch_bounds__(NT) void sk_route_tokens(RouteArgs A, RoutePlan P) 
         }
         sum = group_sum<L>(sum);
         if (live) {
-            const float inv = 1.f / sum;
+            const float inv = reciprocal(sum);
 #pragma unroll
             for (int v = 0; v < V; ++v) psum[v] += ex[v] * inv;
             const float lse = mx + lg2(sum) * kLn2;
@@ -304,9 +307,9 @@ __global__ __launch_bounds__(NT) void sk_route_tokens(RouteArgs A, RoutePlan P) 
             const float u = my_expert >= 0 ? ex2((my_logit - top) * kLog2e) : 0.f;
             const float all = group_sum<L>(u);
             // The row's own sum is used for NaN alone: a NaN logit is never chosen, and its row must not look sound.
-            w = my_expert >= 0 ? (sum != sum ? sum : u / all) : 0.f;
+            w = my_expert >= 0 ? (sum != sum ? sum : u * reciprocal(all)) : 0.f;
         } else {
-            w = my_expert >= 0 ? ex2((my_logit - mx) * kLog2e) / sum : 0.f;
+            w = my_expert >= 0 ? ex2((my_logit - mx) * kLog2e) * reciprocal(sum) : 0.f;
         }
         if (here && lane < k) {
             A.weights[t * k + lane] = w;
@@ -477,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void sk_route_bwd(RouteBwdArgs A) {
         load_logits<T, L, V, VEC>(static_cast<const T *>(A.logits) + tt * E, E, first, x);
         const float mx = A.state[2 * tt], sum = A.state[2 * tt + 1];
         const bool live = mx != neg_inf();
-        const float inv = 1.f / sum, lse = mx + lg2(sum) * kLn2;
+        const float inv = reciprocal(sum), lse = mx + lg2(sum) * kLn2;
         float p[V], pc = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
