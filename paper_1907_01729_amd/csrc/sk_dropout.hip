@@ -43,43 +43,39 @@ __device__ __forceinline__ void drop8(float (&v)[8], uint64_t block, const DropA
     }
 }
 
-// One thread per block of eight elements.  VEC: every pointer is aligned to 16 bytes; the last block may be short.
-template <class T, bool VEC, bool RES>
+// One thread per block of eight elements; the last block may be short.
+template <class T, bool RES>
 __global__ __launch_bounds__(kThreads) void sk_dropout_kernel(const T *x, const T *res, T *y, int64_t n, DropArgs d) {
     const int64_t block = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int64_t i0 = block * 8;
     if (i0 >= n) return;
+    const bool whole = i0 + 8 <= n;
+    const int left = whole ? 8 : (int)(n - i0);
     float v[8], r[8];
-    if (VEC && i0 + 8 <= n) {
+    if (whole) {
         load8(x + i0, v);
         if (RES) load8(res + i0, r);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = i0 + i < n ? (float)x[i0 + i] : 0.f;
-            if (RES) r[i] = i0 + i < n ? (float)res[i0 + i] : 0.f;
-        }
+        load_some(x + i0, 0, left, v);
+        if (RES) load_some(res + i0, 0, left, r);
     }
     drop8(v, block, d);
     if (RES) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
-    if (VEC && i0 + 8 <= n) {
+    if (whole)
         store8(y + i0, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i0 + i < n) y[i0 + i] = (T)v[i];
-    }
+    else
+        store_some(y + i0, 0, left, v);
 }
 
 // A slot outside [0, rows) names no row.
 __device__ __forceinline__ bool names_row(int32_t slot, int64_t rows) { return slot >= 0 && slot < rows; }
 
-// One thread per block of eight elements of y.  VEC: D is a multiple of 8 and every pointer is aligned to 16 bytes,
-// so that a block lies in one row; otherwise each element is on its own.
-template <class T, bool VEC>
+// One thread per block of eight elements of y.  A block that lies in one row goes as a whole; one that does not (D no
+// multiple of eight, or the last block) element by element.
+template <class T>
 __global__ __launch_bounds__(kThreads) void sk_combine_fwd(CombineArgs A) {
     const int64_t n = (int64_t)A.T * A.D, rows = (int64_t)A.T * A.k;
     const int64_t block = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -87,10 +83,10 @@ __global__ __launch_bounds__(kThreads) void sk_combine_fwd(CombineArgs A) {
     if (i0 >= n) return;
     const T *z = static_cast<const T *>(A.z), *res = static_cast<const T *>(A.residual);
     T *y = static_cast<T *>(A.y);
+    const int64_t t = i0 / A.D, col = i0 - t * A.D;
+    const bool whole = col + 8 <= A.D;
     float v[8] = {};
-    if (VEC) {
-        const int64_t t = i0 / A.D;
-        const int64_t col = i0 - t * A.D;
+    if (whole) {
         for (int j = 0; j < A.k; ++j) {
             const int32_t s = A.slots[t * A.k + j];
             if (!names_row(s, rows)) continue;
@@ -101,35 +97,38 @@ __global__ __launch_bounds__(kThreads) void sk_combine_fwd(CombineArgs A) {
             for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(w, a[i], v[i]);
         }
     } else {
-        for (int i = 0; i < 8 && i0 + i < n; ++i) {
-            const int64_t t = (i0 + i) / A.D;
-            const int64_t col = i0 + i - t * A.D;
-            float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i0 + i >= n) continue;
+            const int64_t ti = (i0 + i) / A.D, ci = i0 + i - ti * A.D;
             for (int j = 0; j < A.k; ++j) {
-                const int32_t s = A.slots[t * A.k + j];
+                const int32_t s = A.slots[ti * A.k + j];
                 if (names_row(s, rows))
-                    sum = __builtin_fmaf(A.weights[t * A.k + j], (float)z[(int64_t)s * A.D + col], sum);
+                    v[i] = __builtin_fmaf(A.weights[ti * A.k + j], (float)z[(int64_t)s * A.D + ci], v[i]);
             }
-            v[i] = sum;
         }
     }
     if (A.drop.threshold) drop8(v, block, A.drop);
-    if (VEC) {
-        if (res) {
-            float r[8];
+    const int left = i0 + 8 <= n ? 8 : (int)(n - i0);
+    if (res) {
+        float r[8];
+        if (left == 8)
             load8(res + i0, r);
+        else
+            load_some(res + i0, 0, left, r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
-        }
-        store8(y + i0, v);
-    } else {
-        for (int i = 0; i < 8 && i0 + i < n; ++i) y[i0 + i] = (T)(v[i] + (res ? (float)res[i0 + i] : 0.f));
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
+    if (left == 8)
+        store8(y + i0, v);
+    else
+        store_some(y + i0, 0, left, v);
 }
 
-// One wavefront per token: gy's row is read and dropped out once, then goes to every slot's row and product.  The
-// rows that no slot names (from *used on) are zeroed by the same wavefronts.  KS: slots per pass (registers).
-template <class T, bool VEC, int KS>
+// One wavefront per token, its lanes over the generator's blocks that the token's row meets: gy's row is read and
+// dropped out once, then goes to the rows and products of up to KS slots at a time (their sums are in registers).  The
+// rows that no slot names (from *used on) are zeroed by the same wavefronts.
+template <class T, int KS>
 __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
     const int64_t rows = (int64_t)A.T * A.k;
     const int lane = threadIdx.x & 63;
@@ -137,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
     if (t >= A.T) return;
     const T *z = static_cast<const T *>(A.z), *gy = static_cast<const T *>(A.gy);
     T *gz = static_cast<T *>(A.gz);
-    const int D = A.D;
+    const int64_t D = A.D, first = t * D, last = first + D;  // elements of the row
     for (int j0 = 0; j0 < A.k; j0 += KS) {
         int32_t slot[KS];
         float w[KS], dot[KS];
@@ -149,45 +148,34 @@ __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
             if (!names_row(slot[j], rows)) slot[j] = -1;
             dot[j] = 0.f;
         }
-        if (VEC) {
-            for (int c = lane * 8; c < D; c += 64 * 8) {
-                float g[8];
-                load8(gy + t * D + c, g);
-                if (A.drop.threshold) drop8(g, (uint64_t)(t * D + c) / 8, A.drop);
+        for (int64_t block = first / 8 + lane; block * 8 < last; block += 64) {
+            const int64_t i0 = block * 8, col = i0 - first;  // col < 0: the block begins in the row before
+            const bool whole = col >= 0 && col + 8 <= D;
+            const int lo = col < 0 ? (int)-col : 0, hi = col + 8 <= D ? 8 : (int)(D - col);
+            float g[8];
+            if (whole)
+                load8(gy + i0, g);
+            else
+                load_some(gy + i0, lo, hi, g);
+            if (A.drop.threshold) drop8(g, (uint64_t)block, A.drop);
 #pragma unroll
-                for (int j = 0; j < KS; ++j) {
-                    if (slot[j] < 0) continue;
-                    const int64_t at = (int64_t)slot[j] * D + c;
-                    float a[8], o[8];
+            for (int j = 0; j < KS; ++j) {
+                if (slot[j] < 0) continue;
+                const int64_t at = slot[j] * D + col;
+                float a[8], o[8];
+                if (whole)
                     load8(z + at, a);
+                else
+                    load_some(z + at, lo, hi, a);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dot[j] = __builtin_fmaf(g[i], a[i], dot[j]);
-                        o[i] = w[j] * g[i];
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    dot[j] = __builtin_fmaf(g[i], a[i], dot[j]);
+                    o[i] = w[j] * g[i];
+                }
+                if (whole)
                     store8(gz + at, o);
-                }
-            }
-        } else {
-            // Blocks of the generator do not begin with rows here: each lane draws the block of its element.
-            for (int c = lane; c < D; c += 64) {
-                const int64_t i = t * D + c;
-                float g = (float)gy[i];
-                if (A.drop.threshold) {
-                    float v[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-                    drop8(v, (uint64_t)i / 8, A.drop);
-                    float keep = 0.f;
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) keep = (i & 7) == q ? v[q] : keep;
-                    g = keep > 0.f ? g * keep : 0.f;
-                }
-#pragma unroll
-                for (int j = 0; j < KS; ++j) {
-                    if (slot[j] < 0) continue;
-                    const int64_t at = (int64_t)slot[j] * D + c;
-                    dot[j] = __builtin_fmaf(g, (float)z[at], dot[j]);
-                    gz[at] = (T)(w[j] * g);
-                }
+                else
+                    store_some(gz + at, lo, hi, o);
             }
         }
 #pragma unroll
@@ -199,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
     int64_t used = *A.used;
     used = used < 0 ? 0 : used;
     for (int64_t r = used + t; r < rows; r += A.T)
-        for (int c = lane; c < D; c += 64) gz[r * D + c] = (T)0.f;
+        for (int64_t c = lane; c < D; c += 64) gz[r * D + c] = (T)0.f;
 }
 
 }  // namespace
@@ -208,7 +196,6 @@ hipError_t launch_dropout(const void *x, const void *residual, void *y, int64_t 
                           hipStream_t st) {
     if (n == 0) return hipSuccess;
     const dim3 grid((unsigned)((n + 8 * kThreads - 1) / (8 * kThreads)));
-    const bool vec = aligned16(x) && aligned16(y) && (!residual || aligned16(residual));
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
         auto go = [&](auto kernel) {
@@ -216,8 +203,7 @@ hipError_t launch_dropout(const void *x, const void *residual, void *y, int64_t 
                                static_cast<const T *>(residual), static_cast<T *>(y), n, d);
             return hipGetLastError();
         };
-        if (vec) return residual ? go(sk_dropout_kernel<T, true, true>) : go(sk_dropout_kernel<T, true, false>);
-        return residual ? go(sk_dropout_kernel<T, false, true>) : go(sk_dropout_kernel<T, false, false>);
+        return residual ? go(sk_dropout_kernel<T, true>) : go(sk_dropout_kernel<T, false>);
     });
 }
 
@@ -225,13 +211,9 @@ hipError_t launch_combine_forward(const CombineArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
     const int64_t n = (int64_t)a.T * a.D;
     const dim3 grid((unsigned)((n + 8 * kThreads - 1) / (8 * kThreads)));
-    const bool vec = a.D % 8 == 0 && aligned16(a.z) && aligned16(a.y) && (!a.residual || aligned16(a.residual));
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        if (vec)
-            hipLaunchKernelGGL((sk_combine_fwd<T, true>), grid, dim3(kThreads), 0, st, a);
-        else
-            hipLaunchKernelGGL((sk_combine_fwd<T, false>), grid, dim3(kThreads), 0, st, a);
+        hipLaunchKernelGGL(sk_combine_fwd<T>, grid, dim3(kThreads), 0, st, a);
         return hipGetLastError();
     });
 }
@@ -239,15 +221,10 @@ hipError_t launch_combine_forward(const CombineArgs &a, hipStream_t st) {
 hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
     const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4));
-    const bool vec = a.D % 8 == 0 && aligned16(a.z) && aligned16(a.gy) && aligned16(a.gz);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a);
-            return hipGetLastError();
-        };
-        if (vec) return go(sk_combine_bwd<T, true, 4>);
-        return go(sk_combine_bwd<T, false, 4>);
+        hipLaunchKernelGGL((sk_combine_bwd<T, 4>), grid, dim3(kThreads), 0, st, a);
+        return hipGetLastError();
     });
 }
 

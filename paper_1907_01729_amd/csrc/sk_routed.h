@@ -59,38 +59,37 @@ struct alignas(16) Words4 {
     uint32_t w[4];
 };
 
-template <class T>
-__device__ __forceinline__ float to_float(T v) {
-    return (float)v;
-}
-
-// Eight consecutive elements as 32-bit floats; p is aligned to 16 bytes.
+// Eight consecutive elements as 32-bit floats, at any alignment (the memory takes 16 bytes from anywhere).
 template <class T>
 __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-        typedef T T8 __attribute__((ext_vector_type(8)));
-        const T8 a = *reinterpret_cast<const T8 *>(p);
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    T8 a;
+    __builtin_memcpy(&a, p, sizeof(a));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
 }
 
 // The one rounding of a result held in 32 bits to its type, to nearest even.
 template <class T>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        typedef T T8 __attribute__((ext_vector_type(8)));
-        T8 a;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    T8 a;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = (T)v[i];
-        *reinterpret_cast<T8 *>(p) = a;
-    }
+    for (int i = 0; i < 8; ++i) a[i] = (T)v[i];
+    __builtin_memcpy(p, &a, sizeof(a));
+}
+
+// The same for the elements [lo, hi) of the eight; the others are 0 and stay.
+template <class T>
+__device__ __forceinline__ void load_some(const T *p, int lo, int hi, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i >= lo && i < hi ? (float)p[i] : 0.f;
+}
+template <class T>
+__device__ __forceinline__ void store_some(T *p, int lo, int hi, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i >= lo && i < hi) p[i] = (T)v[i];
 }
 
 // Calls f with a value of the element type of dtype (an sk_dtype).
