@@ -524,36 +524,32 @@ __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
     *reinterpret_cast<T2 *>(static_cast<T *>(A.out) + (int64_t)(t.begin + r) * N + c0 + c) = out;
 }
 
-// gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here.  Eight elements of gx to a
-// thread; VEC: K is a multiple of eight and gx aligned to 16 bytes, so that they lie in one row.
-template <class T, bool VEC>
+// gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here; eight columns to a thread.
+template <class T>
 __global__ __launch_bounds__(kThreads) void sk_experts_sum_slots(ExpertArgs A, const float *rows, T *gx) {
-    const int64_t n = (int64_t)A.T * A.K, all = (int64_t)A.T * A.k;
-    const int64_t i0 = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8;
-    if (i0 >= n) return;
-    if (VEC) {
-        const int64_t t = i0 / A.K, c = i0 - t * A.K;
-        float sum[8] = {};
-        for (int s = 0; s < A.k; ++s) {
-            const int32_t r = A.slots[t * A.k + s];
-            if (r < 0 || r >= all) continue;
-            float v[8];
-            load8(rows + (int64_t)r * A.K + c, v);
+    const int64_t chunks = (A.K + 7) / 8, all = (int64_t)A.T * A.k;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t t = i / chunks, c = (i - t * chunks) * 8;
+    if (t >= A.T) return;
+    const bool whole = c + 8 <= A.K;
+    const int left = whole ? 8 : (int)(A.K - c);
+    float sum[8] = {};
+    for (int s = 0; s < A.k; ++s) {
+        const int32_t r = A.slots[t * A.k + s];
+        if (r < 0 || r >= all) continue;
+        const float *from = rows + (int64_t)r * A.K + c;
+        float v[8];
+        if (whole)
+            load8(from, v);
+        else
+            load_some(from, 0, left, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];
-        }
-        store8(gx + i0, sum);
-    } else {
-        for (int64_t i = i0; i < i0 + 8 && i < n; ++i) {
-            const int64_t t = i / A.K, c = i - t * A.K;
-            float sum = 0.f;
-            for (int s = 0; s < A.k; ++s) {
-                const int32_t r = A.slots[t * A.k + s];
-                if (r >= 0 && r < all) sum += rows[(int64_t)r * A.K + c];
-            }
-            gx[i] = (T)sum;
-        }
+        for (int j = 0; j < 8; ++j) sum[j] += v[j];
     }
+    if (whole)
+        store8(gx + t * A.K + c, sum);
+    else
+        store_some(gx + t * A.K + c, 0, left, sum);
 }
 
 // The parts of a weight gradient, summed in order; n elements, a multiple of eight, eight to a thread.
@@ -706,14 +702,10 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
     if (e != hipSuccess) return e;
     return with_half(a.dtype, [&](auto type) {
         using T = decltype(type);
-        const dim3 grid((unsigned)(((int64_t)a.T * a.K + 8 * kThreads - 1) / (8 * kThreads)));
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a, static_cast<const float *>(ws),
-                               static_cast<T *>(a.out));
-            return hipGetLastError();
-        };
-        return a.K % 8 == 0 && aligned16(ws) && aligned16(a.out) ? go(sk_experts_sum_slots<T, true>)
-                                                                 : go(sk_experts_sum_slots<T, false>);
+        const dim3 grid((unsigned)parts_of((int64_t)a.T * parts_of(a.K, 8), kThreads));
+        hipLaunchKernelGGL((sk_experts_sum_slots<T>), grid, dim3(kThreads), 0, st, a, static_cast<const float *>(ws),
+                           static_cast<T *>(a.out));
+        return hipGetLastError();
     });
 }
 
