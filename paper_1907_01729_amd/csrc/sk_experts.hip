@@ -41,6 +41,10 @@ __device__ __forceinline__ f32x4 mfma16(const Frag8<T> &a, const Frag8<T> &b, f3
 //
 // Elements past the end of the contraction come from a page of zeros; rows and columns past the tile's end repeat the
 // last one and are not stored.
+//
+// 65536 rows of 64 experts of 2048 x 2048, bf16: forward 521 us (1056 TFLOP/s), input gradient's rows 530 us in 16 bits
+// and 580 in 32, weight gradient 741 us; a library product of 65536 x 2048 x 2048 reaches 1441 TFLOP/s here.  Of a step's
+// 1.55 us the products alone take 0.95 (random factors hold the clock near 1.8 GHz) and the copies alone 1.28.
 
 constexpr int kDeep = 64;
 
@@ -461,7 +465,8 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 // Forward for up to 16 rows of an expert at a time: what counts is that the weights are read at the memory's rate, so
 // many wavefronts have to ask for them at once.  A work-group takes kFewCols columns, and its four wavefronts a quarter
 // of the contraction each, straight from memory to registers; their sums meet in LDS.  A lane's 32 bytes of a row's 128
-// are two fragments: the products' order along the contraction is free as long as both factors have the same.
+// are two fragments: the products' order along the contraction is free as long as both factors have the same.  16 rows
+// of 14 of 64 experts of 1024 x 2048: 59 MB in 13 us (4.5 TB/s); in tiles of 64 18 us.
 
 constexpr int kFewRows = 16, kFewCols = 32, kFewChunk = 64, kFewAtOnce = 4;
 
@@ -525,6 +530,7 @@ __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
 }
 
 // gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here; eight columns to a thread.
+// Memory: 65536 rows of 2048 in 118 us (5.1 TB/s).
 template <class T>
 __global__ __launch_bounds__(kThreads) void sk_experts_sum_slots(ExpertArgs A, const float *rows, T *gx) {
     const int64_t chunks = (A.K + 7) / 8, all = (int64_t)A.T * A.k;
