@@ -337,7 +337,8 @@ SK_API int32_t sinkhorn_regime(const sk_problem *p);
  * conventions at the top of this file hold.  Indices that are to come from the
  * router (offsets, tokens, slots) are held to their ranges by the kernels: with
  * others no call reads or writes outside its arrays, but results are
- * unspecified.
+ * unspecified.  But a slot may be set to -1: that leaves its pair out of the
+ * combination and of both gradients that are taken through the slots.
  */
 typedef enum { SK_F32 = 0, SK_BF16 = 1, SK_F16 = 2 } sk_dtype;
 
@@ -459,17 +460,19 @@ typedef struct {
 /*
  * Combination of expert rows with dropout (as above over y, p = 0: none):
  *   y[t] = residual[t] + scale keep sum_s weights[t, s] z[slots[t, s]],
- * z [T k, D], weights [T, k], slots [T, k] as from the router (pairs with slot
- * -1 add nothing), residual [T, D] or NULL, y [T, D].
+ * z [T k, D], weights [T, k], slots [T, k] as from the router, residual [T, D]
+ * or NULL, y [T, D].  Pairs with slot -1 add nothing, those among them whose
+ * slot the caller has set to -1 to leave them out (a limit on an expert's rows).
  */
 SK_API sk_status sinkhorn_combine_forward(const sk_combine *c, const void *z, const float *weights,
                                           const int32_t *slots, const void *residual, void *y, double p,
                                           uint64_t seed, uint64_t offset, void *stream);
 
 /*
- * Its gradients: grad_z [T k, D] (0 in the rows from *used_rows on, which no
- * slot names: used_rows is the router's offsets + E, a device pointer) and
- * grad_weights [T, k] (0 for pairs without a row); the residual's is grad_y.
+ * Its gradients: grad_z [T k, D] (0 in the rows that no slot names: those from
+ * *used_rows on, the router's offsets + E, a device pointer, and those below
+ * whose pair was left out) and grad_weights [T, k] (0 for pairs without a row;
+ * it holds pairs' numbers on the way); the residual's is grad_y.
  */
 SK_API sk_status sinkhorn_combine_backward(const sk_combine *c, const void *z, const float *weights,
                                            const int32_t *slots, const int32_t *used_rows, const void *grad_y,

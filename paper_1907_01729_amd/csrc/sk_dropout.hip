@@ -127,9 +127,21 @@ __global__ __launch_bounds__(kThreads) void sk_combine_fwd(CombineArgs A) {
         store_some(y + i0, 0, left, v);
 }
 
+// The pair that names a row, for every row that one does: pair_of[slots[i]] = i.  The other places keep what they had,
+// so a reader looks whether the pair that it finds there names the row.
+__global__ __launch_bounds__(kThreads) void sk_combine_pairs(const int32_t *slots, int64_t rows, float *pair_of) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= rows) return;
+    const int32_t s = slots[i];
+    if (names_row(s, rows)) pair_of[s] = __int_as_float((int32_t)i);
+}
+
 // One wavefront per token, its lanes over the generator's blocks that the token's row meets: gy's row is read and
-// dropped out once, then goes to the rows and products of up to KS slots at a time (their sums are in registers).  The
-// rows that no slot names (from *used on) are zeroed by the same wavefronts.
+// dropped out once, then goes to the rows and products of up to KS slots at a time (their sums are in registers).
+//
+// The rows that no slot names are zeroed: those from *used on and those whose pair was left out (slot -1).  The pairs
+// that name rows (above) stand in g_weights until the results do: token t's wavefront sees to the rows t k .. t k + k,
+// whose places there are the ones that it alone writes.
 template <class T, int KS>
 __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
     const int64_t rows = (int64_t)A.T * A.k;
@@ -139,6 +151,16 @@ __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
     const T *z = static_cast<const T *>(A.z), *gy = static_cast<const T *>(A.gy);
     T *gz = static_cast<T *>(A.gz);
     const int64_t D = A.D, first = t * D, last = first + D;  // elements of the row
+    bool clear = false;  // lane j: row t k + j
+    if (lane < A.k) {
+        const int64_t r = t * A.k + lane;
+        clear = r >= *A.used;
+        if (!clear) {
+            const int32_t pair = __float_as_int(A.g_weights[r]);
+            clear = !names_row(pair, rows) || A.slots[pair] != r;
+        }
+    }
+    uint64_t cleared = __builtin_amdgcn_ballot_w64(clear);
     for (int j0 = 0; j0 < A.k; j0 += KS) {
         int32_t slot[KS];
         float w[KS], dot[KS];
@@ -186,10 +208,16 @@ __global__ __launch_bounds__(kThreads) void sk_combine_bwd(CombineArgs A) {
             if (lane == 0 && j0 + j < A.k) A.g_weights[t * A.k + j0 + j] = sum;
         }
     }
-    int64_t used = *A.used;
-    used = used < 0 ? 0 : used;
-    for (int64_t r = used + t; r < rows; r += A.T)
-        for (int64_t c = lane; c < D; c += 64) gz[r * D + c] = (T)0.f;
+    for (; cleared; cleared &= cleared - 1) {
+        T *row = gz + (t * A.k + __builtin_ctzll(cleared)) * D;
+        const float none[8] = {};
+        for (int64_t c = lane * 8; c < D; c += 64 * 8) {
+            if (c + 8 <= D)
+                store8(row + c, none);
+            else
+                store_some(row + c, 0, (int)(D - c), none);
+        }
+    }
 }
 
 }  // namespace
@@ -222,6 +250,11 @@ hipError_t launch_combine_forward(const CombineArgs &a, hipStream_t st) {
 
 hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
+    const int64_t rows = (int64_t)a.T * a.k;
+    hipLaunchKernelGGL(sk_combine_pairs, dim3((unsigned)((rows + kThreads - 1) / kThreads)), dim3(kThreads), 0, st,
+                       a.slots, rows, a.g_weights);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4));
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);

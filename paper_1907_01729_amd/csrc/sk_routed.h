@@ -44,7 +44,7 @@ hipError_t launch_dropout(const void *x, const void *residual, void *y, int64_t 
 struct CombineArgs {
     const void *z, *residual, *gy;  // residual may be null
     const float *weights;
-    const int32_t *slots, *used;  // used: device pointer to the number of rows that some slot names
+    const int32_t *slots, *used;  // used: device pointer to the number of experts' rows
     void *y, *gz;
     float *g_weights;
     int T, D, k, dtype;

@@ -448,7 +448,8 @@ def _run_combine(z, weights, slots, residual, T, D, k, counter):
 
 @_on_stream
 def sinkhorn_combine_backward(z, weights, slots, offsets, grad_y, p=0.0, seed=0, offset=0):
-    """(grad_z [T k, D], grad_weights [T, k]); offsets as from the router (its last entry: the rows in use)."""
+    """(grad_z [T k, D], grad_weights [T, k]); offsets as from the router (its last entry: the rows in use).  Rows that
+    no slot names have no gradient."""
     T, D, k = _combine_sizes(z, weights, slots)
     _match(grad_y, "grad_y", z, (T, D), z.dtype)
     _used(offsets, z)
@@ -488,8 +489,8 @@ class _Combine(torch.autograd.Function):
 
 def sinkhorn_expert_combine(z, weights, slots, offsets, residual=None, p=0.0, seed=0, offset=0):
     """residual + dropout(weighted sum of each token's expert rows), [T, D]; differentiable with respect to z
-    [T k, D], weights [T, k] and residual.  slots and offsets are a Routing's; p, seed and offset as in
-    sinkhorn_dropout, over the elements of the result."""
+    [T k, D], weights [T, k] and residual.  slots and offsets are a Routing's, where a slot set to -1 leaves its pair
+    out (a limit on an expert's rows); p, seed and offset as in sinkhorn_dropout, over the elements of the result."""
     z, weights = z.contiguous(), weights.contiguous()
     T, D, k = sizes = _combine_sizes(z, weights, slots)
     wants = z.requires_grad or weights.requires_grad
