@@ -17,6 +17,7 @@ import functools
 from typing import NamedTuple
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, load_library
@@ -78,13 +79,34 @@ def _call(fn, dev, *args):
         raise SinkhornError(status, fn.__name__)
 
 
+def _forward_mode():
+    """Within a level of forward-mode differentiation.  Asked instead of every input's tangent, which takes a third of
+    a microsecond each."""
+    return getattr(forward_ad, "_current_level", 0) >= 0
+
+
+def _recorded(*inputs):
+    """Whether a call goes through autograd: where a gradient of an input is wanted, and in forward mode, where autograd
+    refuses an input with a tangent (the operators have no such derivative, and a result without one would pass for
+    zero).  A call that goes past it saves ten microseconds."""
+    if _forward_mode():
+        return True
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
 def _first_order(fn):
-    """A backward pass that has no derivative itself: who asks for one gets an error.  Only where a graph is built for
-    it, since the wrapper takes ten microseconds of a backward pass."""
+    """A backward pass that has no derivative itself: who asks for one gets an error, in forward mode too.  Only where a
+    graph is built for it, since the wrapper takes ten microseconds of a backward pass."""
     refuses = once_differentiable(fn)
 
     @functools.wraps(fn)
     def backward(ctx, *grads):
+        if _forward_mode() and any(g is not None and forward_ad.unpack_dual(g).tangent is not None for g in grads):
+            raise NotImplementedError("routed layers: the gradients have no derivative in forward mode AD")
         return refuses(ctx, *grads) if torch.is_grad_enabled() else fn(ctx, *grads)
     return backward
 
@@ -229,7 +251,7 @@ def sinkhorn_route(logits, k, bias=None, mask=None, renormalize=True) -> Routing
     logits = logits.contiguous()
     bias = None if bias is None else bias.detach().contiguous()
     mask = None if mask is None else mask.contiguous()
-    if logits.requires_grad and torch.is_grad_enabled():
+    if _recorded(logits):
         return Routing(*_Route.apply(logits, k, bias, mask, renormalize))
     return _route_forward(logits, k, bias, mask, renormalize, False)[0]
 
@@ -372,7 +394,7 @@ def sinkhorn_expert_product(x, weight, offsets, tokens=None, slots=None):
     if slots is not None:
         T, k = sizes[:2]
         _match(slots, "slots", x, (T, k) if T else (0, *slots.shape[1:2]), torch.int32)
-    if (x.requires_grad or weight.requires_grad) and torch.is_grad_enabled():
+    if _recorded(x, weight):
         return _ExpertProduct.apply(x, weight, offsets, tokens, slots, sizes)
     return _run_experts(x, weight, offsets, tokens, sizes)
 
@@ -407,13 +429,11 @@ def sinkhorn_dropout(x, p, seed, offset=0, residual=None):
     nothing, whatever it holds."""
     x = x.contiguous()
     _typed(x, "x")
-    wants = x.requires_grad
     if residual is not None:
         residual = residual.contiguous()
         _match(residual, "residual", x, x.shape, x.dtype)
-        wants = wants or residual.requires_grad
     counter = _counter(p, seed, offset)
-    if wants and torch.is_grad_enabled():
+    if _recorded(x, residual):
         return _Dropout.apply(x, residual, counter)
     return _run_dropout(x, residual, counter)
 
@@ -493,13 +513,11 @@ def sinkhorn_expert_combine(z, weights, slots, offsets, residual=None, p=0.0, se
     out (a limit on an expert's rows); p, seed and offset as in sinkhorn_dropout, over the elements of the result."""
     z, weights = z.contiguous(), weights.contiguous()
     T, D, k = sizes = _combine_sizes(z, weights, slots)
-    wants = z.requires_grad or weights.requires_grad
     if residual is not None:
         residual = residual.contiguous()
         _match(residual, "residual", z, (T, D), z.dtype)
-        wants = wants or residual.requires_grad
     counter = _counter(p, seed, offset)
-    if wants and torch.is_grad_enabled():
+    if _recorded(z, weights, residual):
         _used(offsets, z)
         return _Combine.apply(z, weights, slots, offsets, residual, sizes, counter)
     return _run_combine(z, weights, slots, residual, T, D, k, counter)
