@@ -14,6 +14,8 @@
  *   - Every array argument is a DEVICE pointer to contiguous row-major data
  *     (fp32 unless stated).  The caller owns every buffer; the library never
  *     allocates, frees or synchronises, and keeps no state between calls.
+ *   - Arrays are aligned to their elements, a workspace to 16 bytes (the library
+ *     keeps numbers of 64 bits in it).
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     Work is enqueued asynchronously; results are valid once the stream has
  *     been synchronised.  Calls that overlap on one workspace race.

@@ -208,6 +208,26 @@ def _shapes(mu, nu, C):
     return B, d1, d2, c_batched
 
 
+def _scratch(workspace, need, dev):
+    """At least need bytes on dev for the kernels: the caller's workspace, or new ones where it is None, smaller, or not
+    aligned to the 16 bytes that the library asks for.  The kernels write through its address, so anything but plain
+    memory of that GPU is refused."""
+    if workspace is not None:
+        if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda:
+            raise TypeError("workspace must be a GPU tensor")
+        if workspace.device != dev:
+            raise ValueError(f"workspace must be on {dev}, got {workspace.device}")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        if workspace.numel() * workspace.element_size() >= need and workspace.data_ptr() % 16 == 0:
+            return workspace
+    return torch.empty((max(need, 1),), device=dev, dtype=torch.uint8)
+
+
+def _bytes(workspace):
+    return ctypes.c_size_t(workspace.numel() * workspace.element_size())
+
+
 def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
@@ -243,18 +263,17 @@ def _forward(select, mu, nu, C, lam, n_iter, tol, stream, workspace, alpha0=None
         merr = torch.empty((B,), **f)
         iters = torch.empty((B,), device=dev, dtype=torch.int32)
         need = int(lib.sinkhorn_workspace_bytes(ctypes.byref(p)))
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty((max(need, 1),), device=dev, dtype=torch.uint8)
+        workspace = _scratch(workspace, need, dev)
     if alpha0 is not None:
         st = lib.sinkhorn_forward_warm(ctypes.byref(p), _ptr(alpha0), _ptr(mu), _ptr(nu), _ptr(C), _ptr(alpha),
                                        _ptr(beta), _ptr(loss), _ptr(merr), _ptr(iters), _ptr(workspace),
-                                       ctypes.c_size_t(workspace.numel()), _stream(dev, stream))
+                                       _bytes(workspace), _stream(dev, stream))
         if st != 0:
             raise SinkhornError(st, "sinkhorn_forward_warm")
         return dict(alpha=alpha, beta=beta, loss=loss, marg_err=merr, iters=iters)
     st = lib.sinkhorn_forward_select(ctypes.byref(p), int(select), _ptr(mu), _ptr(nu), _ptr(C), _ptr(alpha),
                                      _ptr(beta), _ptr(loss), _ptr(merr), _ptr(iters), _ptr(workspace),
-                                     ctypes.c_size_t(workspace.numel()), _stream(dev, stream))
+                                     _bytes(workspace), _stream(dev, stream))
     if st != 0:
         raise SinkhornError(st, "sinkhorn_forward" if select == 0 else "sinkhorn_forward_select")
     return dict(alpha=alpha, beta=beta, loss=loss, marg_err=merr, iters=iters)
@@ -371,11 +390,10 @@ def sinkhorn_forward_points(mu, nu, X, Y, lam, n_iter, tol=0.0, stream=None, wor
         merr = torch.empty((B,), **f)
         iters = torch.empty((B,), device=dev, dtype=torch.int32)
         need = int(lib.sinkhorn_points_workspace_bytes(ctypes.byref(p), D))
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty((max(need, 1),), device=dev, dtype=torch.uint8)
+        workspace = _scratch(workspace, need, dev)
     st = lib.sinkhorn_forward_points(ctypes.byref(p), D, _ptr(mu), _ptr(nu), _ptr(X), _ptr(Y), _ptr(alpha),
                                      _ptr(beta), _ptr(loss), _ptr(merr), _ptr(iters), _ptr(workspace),
-                                     ctypes.c_size_t(workspace.numel()), _stream(dev, stream))
+                                     _bytes(workspace), _stream(dev, stream))
     if st != 0:
         raise SinkhornError(st, "sinkhorn_forward_points")
     return dict(alpha=alpha, beta=beta, loss=loss, marg_err=merr, iters=iters)
@@ -429,11 +447,10 @@ def sinkhorn_backward_sharp(grad_loss, mu, nu, C, lam, alpha, beta, max_cg=200, 
         gnu = torch.empty((B, d2), **f)
         its = torch.empty((B,), device=dev, dtype=torch.int32)
         need = int(lib.sinkhorn_sharp_workspace_bytes(ctypes.byref(p)))
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty((max(need, 1),), device=dev, dtype=torch.uint8)
+        workspace = _scratch(workspace, need, dev)
     st = lib.sinkhorn_backward_sharp(ctypes.byref(p), _ptr(grad_loss), _ptr(mu), _ptr(nu), _ptr(C), _ptr(alpha),
                                      _ptr(beta), _ptr(gmu), _ptr(gnu), int(max_cg), ctypes.c_float(cg_tol),
-                                     _ptr(its), _ptr(workspace), ctypes.c_size_t(workspace.numel()),
+                                     _ptr(its), _ptr(workspace), _bytes(workspace),
                                      _stream(dev, stream))
     if st != 0:
         raise SinkhornError(st, "sinkhorn_backward_sharp")

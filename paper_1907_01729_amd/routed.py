@@ -20,7 +20,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
-from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, load_library
+from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, _scratch, load_library
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _HALF = {torch.bfloat16: 1, torch.float16: 2}
@@ -141,12 +141,9 @@ def _combine(T, D, k, dtype):
     return ctypes.byref(SkCombine(T, D, k, dtype))
 
 
-def _scratch(workspace, need, dev):
-    if not need:
-        return None
-    if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty((need,), device=dev, dtype=torch.uint8)
-    return workspace
+def _workspace(workspace, need, dev):
+    """As _scratch, and nothing where nothing is needed or given."""
+    return _scratch(workspace, need, dev) if need or workspace is not None else None
 
 
 def _ptr(t):
@@ -186,7 +183,7 @@ def _route_forward(logits, k, bias, mask, renormalize, with_state, workspace=Non
                                torch.empty((E + 1,), **whole))
     balance, z = torch.empty((), **real), torch.empty((), **real)
     state = torch.empty((2 * T + 1,), **real) if with_state else None
-    scratch = _scratch(workspace, need, dev)
+    scratch = _workspace(workspace, need, dev)
     _call(load_library().sinkhorn_route_forward, dev, r, logits.data_ptr(), _ptr(bias), _ptr(mask),
           weights.data_ptr(), experts.data_ptr(), counts.data_ptr(), offsets.data_ptr(), tokens.data_ptr(),
           slots.data_ptr(), balance.data_ptr(), z.data_ptr(), _ptr(state), _ptr(scratch), need)
@@ -330,7 +327,7 @@ def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspa
 def _run_experts_input(grad_y, weight, offsets, slots, sizes, workspace=None):
     p, need, _ = _experts(*sizes)
     gx = torch.empty((sizes[0], sizes[3]), device=grad_y.device, dtype=grad_y.dtype)
-    scratch = None if slots is None else _scratch(workspace, need, grad_y.device)
+    scratch = None if slots is None else _workspace(workspace, need, grad_y.device)
     _call(load_library().sinkhorn_experts_backward_input, grad_y.device, p, grad_y.data_ptr(), weight.data_ptr(),
           offsets.data_ptr(), _ptr(slots), gx.data_ptr(), _ptr(scratch), need)
     return gx
@@ -359,7 +356,7 @@ def _run_experts_weight(grad_y, x, offsets, tokens, sizes, workspace=None):
     _, _, E, K, N, _ = sizes
     p, _, need = _experts(*sizes)
     gw = torch.empty((E, N, K), device=x.device, dtype=x.dtype)
-    scratch = _scratch(workspace, need, x.device)
+    scratch = _workspace(workspace, need, x.device)
     _call(load_library().sinkhorn_experts_backward_weight, x.device, p, grad_y.data_ptr(), x.data_ptr(),
           offsets.data_ptr(), _ptr(tokens), gw.data_ptr(), _ptr(scratch), need)
     return gw
