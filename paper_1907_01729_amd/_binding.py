@@ -152,8 +152,18 @@ def load_library():
     return lib
 
 
+def _int32(*sizes, status=-2):
+    """The sizes as whole numbers, for fields of 32 bits.  ctypes would cut off what they do not hold, and a call with
+    2^32 + 4 rows would run over four of them."""
+    sizes = tuple(int(n) for n in sizes)
+    for n in sizes:
+        if not -1 << 31 <= n < 1 << 31:
+            raise SinkhornError(status, f"{n} does not fit 32 bits")
+    return sizes
+
+
 def problem(B, d1, d2, c_batched, lam, n_iter, tol=0.0) -> SkProblem:
-    return SkProblem(int(B), int(d1), int(d2), int(c_batched), float(lam), int(n_iter), float(tol))
+    return SkProblem(*_int32(B, d1, d2, c_batched), float(lam), *_int32(n_iter, status=-4), float(tol))
 
 
 def sinkhorn_status_string(status: int) -> str:
@@ -362,12 +372,12 @@ def _point_shapes(mu, nu, X, Y):
     if X.shape[1] != d1 or Y.shape[1] != d2 or X.shape[0] not in (1, B):
         raise ValueError(f"X/Y shapes {tuple(X.shape)} {tuple(Y.shape)} do not match mu/nu")
     c_batched = int(X.shape[0] == B and B != 1)
-    return B, d1, d2, c_batched, int(X.shape[2])
+    return B, d1, d2, c_batched, *_int32(X.shape[2])
 
 
 def sinkhorn_points_workspace_bytes(B, d1, d2, c_batched, D, lam, n_iter, tol=0.0) -> int:
     p = problem(B, d1, d2, c_batched, lam, n_iter, tol)
-    return int(load_library().sinkhorn_points_workspace_bytes(ctypes.byref(p), int(D)))
+    return int(load_library().sinkhorn_points_workspace_bytes(ctypes.byref(p), *_int32(D)))
 
 
 def sinkhorn_forward_points(mu, nu, X, Y, lam, n_iter, tol=0.0, stream=None, workspace=None):
@@ -440,6 +450,7 @@ def sinkhorn_backward_sharp(grad_loss, mu, nu, C, lam, alpha, beta, max_cg=200, 
         _dev(t, n)
     B, d1, d2, cb = _shapes(mu, nu, C)
     p = problem(B, d1, d2, cb, lam, 0, 0.0)
+    max_cg, = _int32(max_cg, status=-4)
     dev = mu.device
     f = dict(device=dev, dtype=torch.float32)
     with _on(stream):
@@ -449,7 +460,7 @@ def sinkhorn_backward_sharp(grad_loss, mu, nu, C, lam, alpha, beta, max_cg=200, 
         need = int(lib.sinkhorn_sharp_workspace_bytes(ctypes.byref(p)))
         workspace = _scratch(workspace, need, dev)
     st = lib.sinkhorn_backward_sharp(ctypes.byref(p), _ptr(grad_loss), _ptr(mu), _ptr(nu), _ptr(C), _ptr(alpha),
-                                     _ptr(beta), _ptr(gmu), _ptr(gnu), int(max_cg), ctypes.c_float(cg_tol),
+                                     _ptr(beta), _ptr(gmu), _ptr(gnu), max_cg, ctypes.c_float(cg_tol),
                                      _ptr(its), _ptr(workspace), _bytes(workspace),
                                      _stream(dev, stream))
     if st != 0:

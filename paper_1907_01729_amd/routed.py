@@ -20,7 +20,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
-from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, _scratch, load_library
+from ._binding import SinkhornError, SkCombine, SkExperts, SkRouter, _dev, _int32, _scratch, load_library
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _HALF = {torch.bfloat16: 1, torch.float16: 2}
@@ -125,20 +125,20 @@ def _on_stream(fn):
 # A call's sizes as the library takes them, and the bytes of workspace they need: functions of the sizes alone.
 @functools.lru_cache(maxsize=1024)
 def _router(T, E, k, dtype, renormalize):
-    r = SkRouter(T, E, k, dtype, renormalize)
+    r = SkRouter(*_int32(T, E, k), dtype, renormalize)
     return ctypes.byref(r), int(load_library().sinkhorn_route_workspace_bytes(ctypes.byref(r)))
 
 
 @functools.lru_cache(maxsize=1024)
 def _experts(T, k, E, K, N, dtype):
-    p = SkExperts(T, k, E, K, N, dtype)
+    p = SkExperts(*_int32(T, k, E, K, N), dtype)
     lib, ref = load_library(), ctypes.byref(p)
     return ref, int(lib.sinkhorn_experts_workspace_bytes(ref)), int(lib.sinkhorn_experts_weight_workspace_bytes(ref))
 
 
 @functools.lru_cache(maxsize=1024)
 def _combine(T, D, k, dtype):
-    return ctypes.byref(SkCombine(T, D, k, dtype))
+    return ctypes.byref(SkCombine(*_int32(T, D, k), dtype))
 
 
 def _workspace(workspace, need, dev):
