@@ -28,8 +28,17 @@ constexpr int kBlocksWanted = 512;
 constexpr int kManyThreads = 1024;
 constexpr uint32_t kNoPair = 0xFFFFFFFFu;
 
-// v_rcp_f32, to one unit in the last place: a full division is ten instructions.
-__device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
+// 1 / x and a / x for x from 1 on: v_rcp_f32, which may be off by a unit in the last place, and one step of Newton's,
+// after which the result is off by little more than half of one (1 / x for x = 1 .. 1024 is the nearest float from any
+// start within a unit, enumerated).  A division that also takes infinities and the smallest numbers is ten instructions.
+__device__ __forceinline__ float reciprocal(float x) {
+    const float r = __builtin_amdgcn_rcpf(x);
+    return __builtin_fmaf(__builtin_fmaf(-x, r, 1.f), r, r);
+}
+__device__ __forceinline__ float quotient(float a, float x) {
+    const float r = __builtin_amdgcn_rcpf(x), q = a * r;
+    return __builtin_fmaf(__builtin_fmaf(-q, x, a), r, q);
+}
 
 // Reductions over aligned groups of L lanes; every lane of the group ends with the same bits.
 template <int L>
@@ -310,9 +319,9 @@ __global__ __launch_bounds__(NT) void sk_route_tokens(RouteArgs A, RoutePlan P) 
             const float u = my_expert >= 0 ? ex2((my_logit - top) * kLog2e) : 0.f;
             const float all = group_sum<L>(u);
             // The row's own sum is used for NaN alone: a NaN logit is never chosen, and its row must not look sound.
-            w = my_expert >= 0 ? (sum != sum ? sum : u * reciprocal(all)) : 0.f;
+            w = my_expert >= 0 ? (sum != sum ? sum : quotient(u, all)) : 0.f;
         } else {
-            w = my_expert >= 0 ? ex2((my_logit - mx) * kLog2e) * reciprocal(sum) : 0.f;
+            w = my_expert >= 0 ? quotient(ex2((my_logit - mx) * kLog2e), sum) : 0.f;
         }
         if (here && lane < k) {
             A.weights[t * k + lane] = w;
