@@ -567,10 +567,14 @@ hipError_t with_shape(int E, bool vec, F f) {
 }
 
 // One block while each group has at most four tokens: two more launches take longer than those in turn.  Beyond, up to
-// 512 blocks, of 1024 threads where 256 would leave a SIMD fewer than eight wavefronts (the k rounds of maxima are one
-// chain of latencies): more blocks would be as many more partial sums for the scan.  65536 tokens, 256 experts, k = 8,
-// tokens and scan, with the maxima still in floats: 512 blocks of 256 threads 118 + 14 us, 2048 of them 80 + 34, 512 of
-// 1024 threads 72 + 9.
+// 512 blocks: more would be as many more partial sums for the scan.  They are of 256 threads, two wavefronts a SIMD, or,
+// from 65 experts on, of 1024: the k rounds of maxima are one chain of latencies, which four wavefronts a SIMD (up to
+// 128 experts, for want of registers) or eight hide.  With up to 64 experts a group is 16 lanes or fewer, and a
+// work-group of 1024 threads has 64 of them or more: its sums over the groups then take longer than the wavefronts
+// save, and want more registers than there are.  Forward, 1024
+// threads / 256, in us: 65536 tokens of 256 experts, k = 8, 71 / 104; of 128, k = 8, 51 / 61; of 100, k = 4, 41 / 48;
+// 20000 of 128, k = 4, 27 / 25; 65536 of 64, k = 8, 37 / 38; of 64, k = 2, 29 / 26; of 16, k = 2, 25 / 21; a million of
+// 64, k = 2, 274 / 173.
 RoutePlan route_plan(int T, int E) {
     RoutePlan P;
     const int L = group_lanes(E);
@@ -580,7 +584,7 @@ RoutePlan route_plan(int T, int E) {
         P.blocks = 1;
         return P;
     }
-    if (E <= 256 && T > kBlocksWanted * P.groups) P.groups = kManyThreads / L;
+    if (E > 64 && E <= 256 && T > kBlocksWanted * P.groups) P.groups = kManyThreads / L;
     const int64_t wanted = (int64_t)kBlocksWanted * P.groups;
     // the pairs of a work-group of 1024 threads: at most 16 KB of LDS
     const int most = P.groups * L == kManyThreads ? kMaxRun * L / 128 : kMaxRun;
@@ -617,7 +621,7 @@ hipError_t launch_route_forward(const RouteArgs &a, hipStream_t st) {
                 return hipGetLastError();
             };
             if (P.blocks == 1) return go(sk_route_tokens<T, L, V, VEC, true, kThreads>);
-            if constexpr (V <= 4) {
+            if constexpr (L >= 32 && V <= 4) {
                 if (P.groups * L == kManyThreads) return go(sk_route_tokens<T, L, V, VEC, false, kManyThreads>);
             }
             return go(sk_route_tokens<T, L, V, VEC, false, kThreads>);
