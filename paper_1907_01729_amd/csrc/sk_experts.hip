@@ -558,19 +558,27 @@ __global__ __launch_bounds__(kThreads) void sk_experts_sum_slots(ExpertArgs A, c
         store_some(gx + t * A.K + c, 0, left, sum);
 }
 
-// The parts of a weight gradient, summed in order; n elements, a multiple of eight, eight to a thread.
+// The parts of a weight gradient, summed in order; n elements, eight to a thread.
 template <class T>
 __global__ __launch_bounds__(kThreads) void sk_experts_sum_parts(const float *part, T *out, int64_t n, int parts) {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8;
     if (i >= n) return;
+    const bool whole = i + 8 <= n;
+    const int left = whole ? 8 : (int)(n - i);
     float sum[8] = {};
     for (int q = 0; q < parts; ++q) {
         float v[8];
-        load8(part + q * n + i, v);
+        if (whole)
+            load8(part + q * n + i, v);
+        else
+            load_some(part + q * n + i, 0, left, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += v[j];
     }
-    store8(out + i, sum);
+    if (whole)
+        store8(out + i, sum);
+    else
+        store_some(out + i, 0, left, sum);
 }
 
 template <class F>
@@ -609,7 +617,7 @@ Cut cut_rows(const ExpertArgs &a, int cols) {
 // where that makes too few work-groups.  Few tiles over many rows are cut along the rows, into parts of eight steps or
 // more, until there are two work-groups a CU.  Measured, in us: 256 / 128: 8192 rows of 8 of 4096 x 2048 197 / 231,
 // 24000 rows of 32 of 2048 x 1024 147 / 174; 128 / 64: 9620 rows of 14 of 96 x 80 16.4 / 10.9; whole / in parts: 65536
-// rows of 16 experts of 512 x 512 111 / 73, 32768 rows of 2 of 128 x 128 131 / 19.
+// rows of 16 experts of 512 x 512 111 / 73, 32768 rows of 2 of 128 x 128 131 / 19, of 128 x 127 809 / 45.
 Cut cut_weight(const ExpertArgs &a) {
     auto tiles = [&](int64_t tile) { return a.E * parts_of(a.N, tile) * parts_of(a.K, tile); };
     if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1};
@@ -683,9 +691,7 @@ hipError_t launch_rows_input(const ExpertArgs &a, hipStream_t st) {
 
 size_t experts_workspace_bytes(int T, int k, int K) { return (size_t)T * k * K * 4; }
 
-// Parts are taken where the sizes allow chunks; whether the pointers do shows in the call, which then needs none.
 size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
-    if (a.K % 8 || a.N % 8) return 0;
     const Cut c = cut_weight(a);
     return c.parts > 1 ? (size_t)c.parts * a.E * a.N * a.K * 4 : 0;
 }
@@ -717,9 +723,7 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
 
 hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st) {
     ExpertArgs r = a;
-    r.parts = 1;
-    Cut c = cut_weight(a);
-    if (!chunks(a) || !aligned16(ws)) c.parts = 1;
+    const Cut c = cut_weight(a);
     r.parts = c.parts;
     r.out32 = c.parts > 1 ? static_cast<float *>(ws) : nullptr;
     const hipError_t e = launch_product<kWeight>(r, c, st);
