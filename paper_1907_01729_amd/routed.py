@@ -266,6 +266,15 @@ def _rows_of(rows, T, name):
     return rows // T
 
 
+def _rows_in_order(rows):
+    """(T, k) for rows that are not gathered, where only T k counts: a token has up to 16 rows, so there are more of
+    them than the library takes tokens."""
+    for k in range(1, 17):
+        if rows <= k << 24 and rows % k == 0:
+            return rows // k, k
+    return rows, 1  # the library refuses it
+
+
 def _half_rows(t, name, cols, ref):
     _typed(t, name, _HALF)
     if t.dim() != 2 or t.shape[1] != cols:
@@ -293,9 +302,11 @@ def _experts_sizes(x, weight, offsets, tokens):
     E, N, K = _weight(weight)
     _half_rows(x, "x", K, weight)
     _match(offsets, "offsets", x, (E + 1,), torch.int32)
-    T, k = x.shape[0], 1
-    if tokens is not None:
+    if tokens is None:
+        T, k = _rows_in_order(x.shape[0])
+    else:
         _match(tokens, "tokens", x, None, torch.int32)
+        T = x.shape[0]
         k = _rows_of(tokens.numel(), T, "tokens")
     return T, k, E, K, N, _HALF[x.dtype]
 
@@ -314,19 +325,22 @@ def sinkhorn_experts_backward_input(grad_y, weight, offsets, slots=None, workspa
     E, N, K = _weight(weight)
     _half_rows(grad_y, "grad_y", N, weight)
     _match(offsets, "offsets", grad_y, (E + 1,), torch.int32)
-    T, k = grad_y.shape[0], 1
-    if slots is not None:
+    rows = grad_y.shape[0]
+    if slots is None:
+        T, k = _rows_in_order(rows)
+    else:
         _match(slots, "slots", grad_y, None, torch.int32)
-        if slots.dim() != 2 or slots.numel() != T:
-            raise ValueError(f"slots must be [T, k] with T k = {T}, got {list(slots.shape)}")
+        if slots.dim() != 2 or slots.numel() != rows:
+            raise ValueError(f"slots must be [T, k] with T k = {rows}, got {list(slots.shape)}")
         T = slots.shape[0]
-        k = _rows_of(slots.numel(), T, "slots")
+        k = _rows_of(rows, T, "slots")
     return _run_experts_input(grad_y, weight, offsets, slots, (T, k, E, K, N, _HALF[grad_y.dtype]), workspace)
 
 
 def _run_experts_input(grad_y, weight, offsets, slots, sizes, workspace=None):
     p, need, _ = _experts(*sizes)
-    gx = torch.empty((sizes[0], sizes[3]), device=grad_y.device, dtype=grad_y.dtype)
+    rows = grad_y.shape[0] if slots is None else sizes[0]
+    gx = torch.empty((rows, sizes[3]), device=grad_y.device, dtype=grad_y.dtype)
     scratch = None if slots is None else _workspace(workspace, need, grad_y.device)
     _call(load_library().sinkhorn_experts_backward_input, grad_y.device, p, grad_y.data_ptr(), weight.data_ptr(),
           offsets.data_ptr(), _ptr(slots), gx.data_ptr(), _ptr(scratch), need)
@@ -343,12 +357,13 @@ def sinkhorn_experts_backward_weight(grad_y, x, offsets, tokens=None, workspace=
     _half_rows(x, "x", K, grad_y)
     _match(offsets, "offsets", x, None, torch.int32)
     E = offsets.numel() - 1
-    k = 1
     if tokens is not None:
         _match(tokens, "tokens", x, (rows,), torch.int32)
         k = _rows_of(rows, T, "tokens")
     elif T != rows:
         raise ValueError(f"without tokens x must have {rows} rows as grad_y, got {T}")
+    else:
+        T, k = _rows_in_order(rows)
     return _run_experts_weight(grad_y, x, offsets, tokens, (T, k, E, K, N, _HALF[x.dtype]), workspace)
 
 
