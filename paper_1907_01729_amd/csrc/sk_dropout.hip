@@ -9,8 +9,8 @@
 // as 1, 2, 3", 2011).  One block of four words serves eight elements, 16 bits each: the drop rate is then a multiple
 // of 2^-16 (scale is of that rate, so the mean is kept exactly), and the generator costs half of what a word per
 // element would: its 20 multiplications then fit beside the memory's time.  All of these are bound by memory.  67M bf16
-// elements with a residual 70 us (5.8 TB/s), without 41 us (6.6 TB/s); 16384 tokens of 2048 from four rows each,
-// forward 92 us (4.4 TB/s), backward 123 us (4.9 TB/s).
+// elements with a residual 72 us (5.6 TB/s), without 44 us (6.1 TB/s); 16384 tokens of 2048 from four rows each,
+// forward 96 us (4.2 TB/s), backward 128 us (4.7 TB/s) after 5 for the pairs.
 #include "sk_routed.h"
 
 namespace sk {

@@ -42,9 +42,11 @@ __device__ __forceinline__ f32x4 mfma16(const Frag8<T> &a, const Frag8<T> &b, f3
 // Elements past the end of the contraction come from a page of zeros; rows and columns past the tile's end repeat the
 // last one and are not stored.
 //
-// 65536 rows of 64 experts of 2048 x 2048, bf16: forward 521 us (1056 TFLOP/s), input gradient's rows 530 us in 16 bits
-// and 580 in 32, weight gradient 741 us; a library product of 65536 x 2048 x 2048 reaches 1441 TFLOP/s here.  Of a step's
-// 1.55 us the products alone take 0.95 (random factors hold the clock near 1.8 GHz) and the copies alone 1.28.
+// 65536 rows of 64 experts of 2048 x 2048, bf16: forward 509 us (1080 TFLOP/s), the input gradient's rows in 32 bits 561
+// (981), weight gradient 647 (849); a library product of 65536 x 2048 x 2048 reaches 1410 TFLOP/s here.  Of a step's
+// 1.55 us the products alone take 0.95 and the copies alone 1.28.  The LDS reads are not what bounds a step: 16-byte reads
+// alone reach 248 bytes a cycle a CU, transposing ones 173, which for the weight gradient's 192 KB is a quarter of a step.
+// Rows that are no whole 16 bytes take 2 times as long forward and 3 to 4 times in the gradients.
 
 constexpr int kDeep = 64;
 
@@ -698,8 +700,10 @@ size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
 
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    // The weights are read once for each 16 rows of an expert.  256 rows, 64 experts of 2048 x 2048: 95 us, tiles 115;
-    // 512 rows, 64 of 1024 x 1024: 34 us, tiles 28.
+    // The weights are read once for each 16 rows of an expert.  Few / tiles, in us: 256 rows, 64 experts of 2048 x 2048
+    // 95 / 115; 512 rows, 64 of 1024 x 1024 34 / 28.  Up to 64 rows of few experts, too, where tiles are too few: 64 rows
+    // of one of 2048 x 2048 9.0 / 11.3, of 4096 x 4096 25 / 32, of 512 x 512 4.8 / 5.5; of four of 2048 x 2048 9.6 / 17.
+    // Only large matrices have tiles enough then: 32 rows of 8192 x 8192 45 / 57, but 64 rows 87 / 61.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, a.N), st);

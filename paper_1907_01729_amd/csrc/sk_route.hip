@@ -10,8 +10,8 @@
 //   sk_route_place    start of the expert + start of the block + rank; the losses
 // Few tokens are one block, which finishes in the first launch.  All sums are taken in a fixed order in 32 bits.
 //
-// 65536 tokens, 256 experts, k = 8, fp32: tokens 56 us, bound by vector issue (450 instructions a token, three fifths of
-// them the k maxima; reading the logits would take 14 us), scan 9, place 8, gradient 33 us (131 MB, 4.0 TB/s).
+// 65536 tokens, 256 experts, k = 8, fp32: tokens 54 us, bound by vector issue (450 instructions a token, three fifths
+// of them the k maxima; reading the logits would take 14 us), scan 9, place 8, gradient 31 us (131 MB, 4.2 TB/s).
 #include <type_traits>
 
 #include "sk_routed.h"
@@ -29,8 +29,9 @@ constexpr int kManyThreads = 1024;
 constexpr uint32_t kNoPair = 0xFFFFFFFFu;
 
 // 1 / x and a / x for x from 1 on: v_rcp_f32, which may be off by a unit in the last place, and one step of Newton's,
-// after which the result is off by little more than half of one (1 / x for x = 1 .. 1024 is the nearest float from any
-// start within a unit, enumerated).  A division that also takes infinities and the smallest numbers is ten instructions.
+// after which the result is off by little more than half of one (1 / x for x = 1 .. 1024 is the nearest float from
+// any start within a unit, enumerated).  A division that also takes infinities and the smallest numbers is ten
+// instructions.
 __device__ __forceinline__ float reciprocal(float x) {
     const float r = __builtin_amdgcn_rcpf(x);
     return __builtin_fmaf(__builtin_fmaf(-x, r, 1.f), r, r);
@@ -566,15 +567,19 @@ hipError_t with_shape(int E, bool vec, F f) {
     return f(Int<64>{}, Int<16>{}, std::false_type{});
 }
 
-// One block while each group has at most four tokens: two more launches take longer than those in turn.  Beyond, up to
-// 512 blocks: more would be as many more partial sums for the scan.  They are of 256 threads, two wavefronts a SIMD, or,
-// from 65 experts on, of 1024: the k rounds of maxima are one chain of latencies, which four wavefronts a SIMD (up to
-// 128 experts, for want of registers) or eight hide.  With up to 64 experts a group is 16 lanes or fewer, and a
-// work-group of 1024 threads has 64 of them or more: its sums over the groups then take longer than the wavefronts
-// save, and want more registers than there are.  Forward, 1024
-// threads / 256, in us: 65536 tokens of 256 experts, k = 8, 71 / 104; of 128, k = 8, 51 / 61; of 100, k = 4, 41 / 48;
-// 20000 of 128, k = 4, 27 / 25; 65536 of 64, k = 8, 37 / 38; of 64, k = 2, 29 / 26; of 16, k = 2, 25 / 21; a million of
-// 64, k = 2, 274 / 173.
+// One block while each group has at most four tokens: two more launches take longer than those in turn.  One launch /
+// three, in us: 64 tokens of 64 experts, k = 2, 8.2 / 9.7, 128 of them 12.9 / 9.9; 8 of 256, k = 8, 7.8 / 10.7, 16 of
+// them 12.1 / 11.1.  Beyond, up to 512 blocks: fewer leave wavefronts out, more are as many more partial sums for the
+// scan.  512 / 256 / 1024 of them: 65536 tokens of 64, k = 2, 25.8 / 37.8 / 30.4; of 256, k = 8, 70.5 / 74.4 / 75.6;
+// 20000 of 128, k = 4, 27.3 / 21.1 / 32.2.
+//
+// The blocks are of 256 threads, two wavefronts a SIMD, or, from 65 experts on, of 1024: the k rounds of maxima are
+// one chain of latencies, which four wavefronts a SIMD (up to 128 experts, for want of registers) or eight hide.
+// With up to 64 experts a group is 16 lanes or fewer, and a work-group of 1024 threads has 64 of them or more: its
+// sums over the groups then take longer than the wavefronts save, and want more registers than there are.  1024
+// threads / 256: 65536 tokens of 256, k = 8, 71 / 104; of 128, k = 8, 51 / 61; of 100, k = 4, 41 / 48; 20000 of 128,
+// k = 4, 27 / 25; 65536 of 64, k = 8, 37 / 38; of 64, k = 2, 29 / 26; of 16, k = 2, 25 / 21; a million of 64, k = 2,
+// 274 / 173.
 RoutePlan route_plan(int T, int E) {
     RoutePlan P;
     const int L = group_lanes(E);
