@@ -481,6 +481,120 @@ SK_API sk_status sinkhorn_combine_backward(const sk_combine *c, const void *z, c
                                            void *grad_z, float *grad_weights, double p, uint64_t seed,
                                            uint64_t offset, void *stream);
 
+/*
+ * The block around a layer: its norms, gate and residual.
+ *   norm(x; w, b)[i] = (x[i] - m) r w[i] + b[i],  r = (mean((x - m)^2) + eps)^-1/2,
+ * over the N columns of a row, with m = mean(x) (SK_NORM_CENTRED) or m = 0
+ * (SK_NORM_RMS); w and b [N] may be NULL (1 and 0).  In 32 bits throughout.
+ */
+typedef enum { SK_NORM_NONE = 0, SK_NORM_RMS = 1, SK_NORM_CENTRED = 2 } sk_norm_kind;
+
+/* Shape of a gate: none, one value a row, one a column, one an element. */
+typedef enum { SK_GATE_NONE = 0, SK_GATE_ROWS = 1, SK_GATE_COLUMNS = 2, SK_GATE_FULL = 3 } sk_gate_kind;
+
+typedef struct {
+    int32_t T, N;       /* rows and columns: 0 <= T <= 2^24, 1 <= N <= 2^16      */
+    int32_t dtype;      /* sk_dtype of all [T, N] arrays but the gate            */
+    int32_t wdtype;     /* of every w and b and their gradients: dtype or SK_F32 */
+    int32_t gate;       /* sk_gate_kind                                          */
+    int32_t gdtype;     /* of the gate and its gradient: dtype or SK_F32         */
+    int32_t after;      /* sk_norm_kind of the block's output                    */
+    int32_t before;     /* sk_norm_kind of the sum, for the next block           */
+    float scale;        /* of the residual, finite                               */
+    float eps_after, eps_before;  /* finite, >= 0                                */
+} sk_norms;
+
+/*
+ * Norm of x [T, N] by p->before (not SK_NORM_NONE) with eps_before; the gate,
+ * `after` and the scale are not used.  stats [T, 4] (may be NULL without a
+ * backward pass) keeps the rows' means and r.
+ */
+SK_API sk_status sinkhorn_norm_forward(const sk_norms *p, const void *x, const void *w, const void *b, void *y,
+                                       float *stats, void *stream);
+
+/*
+ * The end of a block:
+ *   n = norm_after(h)  (h itself where p->after is SK_NORM_NONE),
+ *   out = scale residual + gate n,      rounded to dtype,
+ *   next = norm_before(out)             (of the rounded sum; only where
+ *                                        p->before is not SK_NORM_NONE).
+ * gate [T, 1], [1, N] or [T, N] (p->gate); no array may be another's.
+ */
+SK_API sk_status sinkhorn_residual_norm_forward(const sk_norms *p, const void *h, const void *residual,
+                                                const void *gate, const void *after_w, const void *after_b,
+                                                const void *before_w, const void *before_b, void *out, void *next,
+                                                float *stats, void *stream);
+
+/*
+ * Gradients of both, with stats of the forward pass.  Gradients of w, b and the
+ * gate are summed over the rows (columns) they were broadcast to, in 32 bits and
+ * in a fixed order, through the workspace; any gradient may be NULL: not wanted.
+ * grad_out or grad_next may be NULL: no gradient from there.
+ */
+SK_API size_t sinkhorn_norm_workspace_bytes(const sk_norms *p);
+SK_API sk_status sinkhorn_norm_backward(const sk_norms *p, const void *x, const void *w, const float *stats,
+                                        const void *grad_y, void *grad_x, void *grad_w, void *grad_b,
+                                        void *workspace, size_t ws_bytes, void *stream);
+SK_API sk_status sinkhorn_residual_norm_backward(const sk_norms *p, const void *h, const void *out, const void *gate,
+                                                 const void *after_w, const void *after_b, const void *before_w,
+                                                 const float *stats, const void *grad_out, const void *grad_next,
+                                                 void *grad_h, void *grad_residual, void *grad_gate,
+                                                 void *grad_after_w, void *grad_after_b, void *grad_before_w,
+                                                 void *grad_before_b, void *workspace, size_t ws_bytes,
+                                                 void *stream);
+
+/*
+ * Rows in 8 bits: whole numbers q with a scale s for each row, or for each 128
+ * columns of a row (p->block = 128):
+ *   s = max |x| / 127 over them, rounded to 32 bits,
+ *   q = x / s rounded to nearest, ties to even (of the exact quotient), within
+ *       [-127, 127];  s = 0: q = 0;  infinity or NaN among them: s = NaN, q = 0.
+ * values [rows, P] int8 with P = columns up to whole 16, zeros past the columns,
+ * aligned to 16 bytes (SK_ERR_ARG); scales [rows, ceil(columns / block)] or
+ * [rows] fp32.
+ */
+typedef struct {
+    int64_t rows;    /* 0 <= rows <= 2^26, rows columns <= 2^34 */
+    int32_t columns; /* 1 <= columns <= 2^17                    */
+    int32_t block;   /* 128, or 0: the whole row                */
+    int32_t dtype;   /* sk_dtype of the unpacked rows           */
+} sk_packing;
+
+SK_API sk_status sinkhorn_pack(const sk_packing *p, const void *x, void *values, float *scales, void *stream);
+/* x = s q, rounded to dtype. */
+SK_API sk_status sinkhorn_unpack(const sk_packing *p, const void *values, const float *scales, void *x,
+                                 void *stream);
+
+/*
+ * Activations of rows x [rows, columns]:
+ *   y = act(x) [rows, columns],  or with gated = 1
+ *   y = act(x[:, :K]) x[:, K:]   [rows, K],  columns = 2 K,
+ * act(x) = x, max(x, 0), x / (1 + exp(-x)), x (1 + erf(x / sqrt 2)) / 2.  In 32
+ * bits, one rounding to dtype.  values and scales (p->block = 128; both or none)
+ * receive x in 8 bits, as in sinkhorn_pack.
+ */
+typedef enum { SK_ACT_NONE = 0, SK_ACT_RELU = 1, SK_ACT_SILU = 2, SK_ACT_GELU = 3 } sk_activation;
+SK_API sk_status sinkhorn_activation_forward(const sk_packing *p, int32_t activation, int32_t gated, const void *x,
+                                             void *y, void *values, float *scales, void *stream);
+/*
+ * From x kept in 8 bits, x~ = s q: y = the activation of x~ again (may be NULL)
+ * and grad_x = its derivative at x~ times grad_y (both may be NULL, together).
+ */
+SK_API sk_status sinkhorn_activation_backward(const sk_packing *p, int32_t activation, int32_t gated,
+                                              const void *values, const float *scales, const void *grad_y, void *y,
+                                              void *grad_x, void *stream);
+
+/*
+ * Experts' products of rows in 8 bits: as sinkhorn_experts_forward with
+ *   y[r, n] = xs[src(r)] ws[e, n] sum_k xv[src(r), k] wv[e, n, k],
+ * x packed by rows of K columns (block = 0), w [E, N, K] packed as E N rows; the
+ * sum is a whole number and exact.  p->dtype is y's type, SK_F32 too.  offsets may
+ * be NULL where E = 1: all rows are that expert's.
+ */
+SK_API sk_status sinkhorn_experts_forward_packed(const sk_experts *p, const void *xv, const float *xs,
+                                                 const void *wv, const float *ws, const int32_t *offsets,
+                                                 const int32_t *tokens, void *y, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

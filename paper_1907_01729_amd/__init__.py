@@ -29,6 +29,24 @@ from ._binding import (  # noqa: F401
     sinkhorn_workspace_bytes,
 )
 from .loss import SinkhornLoss, SinkhornPointsLoss, sinkhorn_loss, sinkhorn_loss_points  # noqa: F401
+from .norm import (  # noqa: F401
+    Norm,
+    NormGradients,
+    sinkhorn_norm,
+    sinkhorn_norm_backward,
+    sinkhorn_norm_forward,
+    sinkhorn_residual_norm,
+    sinkhorn_residual_norm_backward,
+    sinkhorn_residual_norm_forward,
+)
+from .packed import (  # noqa: F401
+    Packed,
+    sinkhorn_activation,
+    sinkhorn_expert_product_kept,
+    sinkhorn_expert_product_packed,
+    sinkhorn_pack,
+    sinkhorn_unpack,
+)
 from .routed import (  # noqa: F401
     Routing,
     sinkhorn_combine_backward,
@@ -66,6 +84,20 @@ __all__ = [
     "sinkhorn_sharp_workspace_bytes",
     "sinkhorn_status_string",
     "sinkhorn_workspace_bytes",
+    "Norm",
+    "NormGradients",
+    "sinkhorn_norm",
+    "sinkhorn_norm_backward",
+    "sinkhorn_norm_forward",
+    "sinkhorn_residual_norm",
+    "sinkhorn_residual_norm_backward",
+    "sinkhorn_residual_norm_forward",
+    "Packed",
+    "sinkhorn_activation",
+    "sinkhorn_expert_product_kept",
+    "sinkhorn_expert_product_packed",
+    "sinkhorn_pack",
+    "sinkhorn_unpack",
     "Routing",
     "sinkhorn_combine_backward",
     "sinkhorn_combine_forward",

@@ -51,6 +51,16 @@ EXPORTED = (
     "sinkhorn_dropout",
     "sinkhorn_combine_forward",
     "sinkhorn_combine_backward",
+    "sinkhorn_norm_forward",
+    "sinkhorn_norm_backward",
+    "sinkhorn_norm_workspace_bytes",
+    "sinkhorn_residual_norm_forward",
+    "sinkhorn_residual_norm_backward",
+    "sinkhorn_pack",
+    "sinkhorn_unpack",
+    "sinkhorn_activation_forward",
+    "sinkhorn_activation_backward",
+    "sinkhorn_experts_forward_packed",
 )
 
 
@@ -82,6 +92,15 @@ class SkExperts(ctypes.Structure):
 
 class SkCombine(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "D", "k", "dtype")]
+
+
+class SkNorms(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "N", "dtype", "wdtype", "gate", "gdtype", "after", "before")] + [
+        (n, ctypes.c_float) for n in ("scale", "eps_after", "eps_before")]
+
+
+class SkPacking(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("columns", "block", "dtype")]
 
 
 def library_path() -> str:
@@ -145,8 +164,22 @@ def load_library():
     lib.sinkhorn_dropout.argtypes = [ctypes.c_int64, I, P, P, P, D, U, U, P]
     lib.sinkhorn_combine_forward.argtypes = [PC, P, P, P, P, P, D, U, U, P]
     lib.sinkhorn_combine_backward.argtypes = [PC, P, P, P, P, P, P, P, D, U, U, P]
+    PN, PK = ctypes.POINTER(SkNorms), ctypes.POINTER(SkPacking)
+    lib.sinkhorn_norm_forward.argtypes = [PN, *[P] * 6]
+    lib.sinkhorn_norm_workspace_bytes.argtypes = [PN]
+    lib.sinkhorn_norm_workspace_bytes.restype = Z
+    lib.sinkhorn_norm_backward.argtypes = [PN, *[P] * 8, Z, P]
+    lib.sinkhorn_residual_norm_forward.argtypes = [PN, *[P] * 11]
+    lib.sinkhorn_residual_norm_backward.argtypes = [PN, *[P] * 17, Z, P]
+    lib.sinkhorn_pack.argtypes = [PK, *[P] * 4]
+    lib.sinkhorn_unpack.argtypes = [PK, *[P] * 4]
+    lib.sinkhorn_activation_forward.argtypes = [PK, I, I, *[P] * 5]
+    lib.sinkhorn_activation_backward.argtypes = [PK, I, I, *[P] * 6]
+    lib.sinkhorn_experts_forward_packed.argtypes = [PE, *[P] * 8]
     for name in ("route_forward", "route_backward", "experts_forward", "experts_backward_input",
-                 "experts_backward_weight", "dropout", "combine_forward", "combine_backward"):
+                 "experts_backward_weight", "dropout", "combine_forward", "combine_backward", "norm_forward",
+                 "norm_backward", "residual_norm_forward", "residual_norm_backward", "pack", "unpack",
+                 "activation_forward", "activation_backward", "experts_forward_packed"):
         getattr(lib, "sinkhorn_" + name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -44,16 +44,7 @@ bool drop_args(double p, uint64_t seed, uint64_t offset, sk::DropArgs *d) {
     return true;
 }
 
-sk_status check_experts(const sk_experts *p) {
-    if (!p) return SK_ERR_NULLPTR;
-    if (p->T < 0 || p->T > kMaxTokens || p->k < 1 || p->k > kMaxSlots || p->E < 1 || p->E > kMaxExperts)
-        return SK_ERR_SHAPE;
-    if (p->K < 1 || p->N < 1 || p->K > kMaxColumns || p->N > kMaxColumns) return SK_ERR_SHAPE;
-    const int64_t rows = (int64_t)p->T * p->k, wide = p->K > p->N ? p->K : p->N;
-    if (rows * wide > kMaxElements || (int64_t)p->E * p->N * p->K > kMaxElements) return SK_ERR_SHAPE;
-    if (p->dtype != SK_BF16 && p->dtype != SK_F16) return SK_ERR_ARG;
-    return SK_OK;
-}
+sk_status check_experts(const sk_experts *p) { return sk::check_experts(p, false); }
 
 sk::ExpertArgs expert_args(const sk_experts *p) {
     sk::ExpertArgs a = {};
@@ -67,6 +58,21 @@ sk::ExpertArgs expert_args(const sk_experts *p) {
 }
 
 }  // namespace
+
+namespace sk {
+
+sk_status check_experts(const sk_experts *p, bool packed) {
+    if (!p) return SK_ERR_NULLPTR;
+    if (p->T < 0 || p->T > kMaxTokens || p->k < 1 || p->k > kMaxSlots || p->E < 1 || p->E > kMaxExperts)
+        return SK_ERR_SHAPE;
+    if (p->K < 1 || p->N < 1 || p->K > kMaxColumns || p->N > kMaxColumns) return SK_ERR_SHAPE;
+    const int64_t rows = (int64_t)p->T * p->k, wide = p->K > p->N ? p->K : p->N;
+    if (rows * wide > kMaxElements || (int64_t)p->E * p->N * p->K > kMaxElements) return SK_ERR_SHAPE;
+    return packed ? is_dtype(p->dtype) ? SK_OK : SK_ERR_ARG
+                  : p->dtype == SK_BF16 || p->dtype == SK_F16 ? SK_OK : SK_ERR_ARG;
+}
+
+}  // namespace sk
 
 extern "C" {
 

@@ -16,10 +16,16 @@ struct ExpertArgs {
     float *out32;  // where set, the rows' result in 32 bits goes here instead
     int T, k, E, K, N, dtype;
     int parts;  // weight: parts of the rows
+    // Rows in 8 bits: x and w hold pairs of whole numbers, K counts pairs, dtype is the result's.
+    const float *x_scale, *w_scale;
+    bool whole_out;  // their results are stored in whole 16 bytes
 };
+// packed: of rows in 8 bits, whose results have any type.
+sk_status check_experts(const sk_experts *p, bool packed);
 size_t experts_workspace_bytes(int T, int k, int K);
 size_t experts_weight_workspace_bytes(const ExpertArgs &a);
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st);
+hipError_t launch_experts_packed(const ExpertArgs &a, hipStream_t st);
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st);
 hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st);
 
@@ -27,12 +33,14 @@ template <class T>
 using Frag8 = T __attribute__((ext_vector_type(8)));
 
 // Rows [begin, end) of an expert; e = E: the rows of none.  Whatever the offsets hold, within the rows there are.
+// Without offsets all are the first expert's.
 struct RowRange {
     int begin, end;
 };
 __device__ __forceinline__ RowRange expert_rows(const ExpertArgs &A, int e) {
     const int rows = A.T * A.k;
     RowRange r;
+    if (!A.offsets) return {e ? rows : 0, rows};
     r.begin = min(max(A.offsets[e], 0), rows);
     r.end = e < A.E ? min(max(A.offsets[e + 1], 0), rows) : rows;
     if (r.end < r.begin) r.end = r.begin;

@@ -14,10 +14,22 @@ namespace {
 constexpr int kThreads = 256;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Two neighbouring whole numbers of 8 bits: where the factors are these, the kernels below move them as they move
+// 16-bit factors, and only the products and what becomes of the sums differ.
+using Pair = int16_t;
+template <class T>
+constexpr bool kPairs = std::is_same_v<T, Pair>;
+template <class T>
+using Sum4 = std::conditional_t<kPairs<T>, i32x4, f32x4>;
 
 template <class T>
-__device__ __forceinline__ f32x4 mfma16(const Frag8<T> &a, const Frag8<T> &b, f32x4 c) {
-    if constexpr (std::is_same_v<T, __bf16>)
+__device__ __forceinline__ Sum4<T> mfma16(const Frag8<T> &a, const Frag8<T> &b, Sum4<T> c) {
+    if constexpr (kPairs<T>)
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0,
+                                                     0);
+    else if constexpr (std::is_same_v<T, __bf16>)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -206,7 +218,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     m1 = __builtin_amdgcn_readfirstlane(m1), c0 = __builtin_amdgcn_readfirstlane(c0);
     r0 = __builtin_amdgcn_readfirstlane(r0), deep = __builtin_amdgcn_readfirstlane(deep);
 
-    f32x4 acc[FM][FN] = {};
+    Sum4<T> acc[FM][FN] = {};
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     const bool idle = m0 + wm >= m1 || c0 + wn >= cols;  // the wavefront's part lies past the edge: it copies only
     if (deep > 0) {
@@ -417,6 +429,26 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     // lane % 16, columns (lane / 16) * 4 of a 16 x 16 block), 32 bytes a row of a block.  Written straight from there the
     // products took 6 % longer.  Results in 32 bits go in WM passes, of BM / WM rows.
     __syncthreads();  // nobody reads the last step's operands any more
+    [[maybe_unused]] float x_scale[kPairs<T> ? FM : 1], w_scale[kPairs<T> ? FN : 1][4];
+    if constexpr (kPairs<T>) {
+        static_assert(MODE == kForward && !STAGED);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int r = min(m0 + wm + i * 16 + (lane & 15), m1 - 1);
+            int t = GATHERED ? A.tokens[r] : r;
+            if (GATHERED && (t < 0 || t >= A.T)) t = 0;
+            x_scale[i] = deep > 0 ? A.x_scale[t] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int c = min(c0 + wn + j * 16 + (lane >> 4) * 4 + v, N - 1);
+                w_scale[j][v] = deep > 0 ? A.w_scale[(int64_t)e * N + c] : 0.f;
+            }
+    }
+    // Whether results are stored in whole 16 bytes: rows in 8 bits are, whatever the results' columns.
+    const bool whole_out = !STAGED && (!kPairs<T> || A.whole_out);
     const int64_t row0 = MODE == kWeight ? ((int64_t)part * A.E + e) * N : 0;
     auto pass = [&](auto type, int rows0, int rows, bool mine) {
         using O = decltype(type);
@@ -429,7 +461,12 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                     typedef O O4 __attribute__((ext_vector_type(4)));
                     O4 o;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) o[v] = (O)acc[i][j][v];
+                    for (int v = 0; v < 4; ++v) {
+                        if constexpr (kPairs<T>)
+                            o[v] = (O)((float)acc[i][j][v] * x_scale[i] * w_scale[j][v]);
+                        else
+                            o[v] = (O)acc[i][j][v];
+                    }
                     *reinterpret_cast<O4 *>(lds + (wm - rows0 + i * 16 + (lane & 15)) * kPitch +
                                             (wn + j * 16 + (lane >> 4) * 4) * (int)sizeof(O)) = o;
                 }
@@ -441,7 +478,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             const Words4 v = *reinterpret_cast<const Words4 *>(lds + r * kPitch + c % kChunks * 16);
             char *out = sizeof(O) == 4 ? reinterpret_cast<char *>(A.out32) : static_cast<char *>(A.out);
             out += ((row0 + row) * cols + col) * (int)sizeof(O);
-            if constexpr (!STAGED) {
+            if (whole_out) {
                 *reinterpret_cast<Words4 *>(out) = v;
             } else if (cols - col >= kEach) {
                 __builtin_memcpy(out, &v, 16);
@@ -451,12 +488,17 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             }
         }
     };
-    if (MODE != kForward && A.out32) {
+    if ((MODE != kForward || kPairs<T>) && A.out32) {
 #pragma unroll
         for (int q = 0; q < WM; ++q) {
             if (q) __syncthreads();
             pass(float{}, q * (BM / WM), BM / WM, wm == q * (BM / WM));
         }
+    } else if constexpr (kPairs<T>) {
+        if (A.dtype == SK_BF16)
+            pass(__bf16{}, 0, BM, true);
+        else
+            pass(_Float16{}, 0, BM, true);
     } else {
         pass(T{}, 0, BM, true);
     }
@@ -475,13 +517,14 @@ constexpr int kFewRows = 16, kFewCols = 32, kFewChunk = 64, kFewAtOnce = 4;
 template <class T, bool GATHERED>
 __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
     constexpr int NC = kFewCols / 16, kWaves = kThreads / 64, kPitch = kFewCols + 4;
-    __shared__ __attribute__((aligned(16))) float part[kWaves][kFewRows][kPitch];
+    using Sum = std::conditional_t<kPairs<T>, int, float>;
+    __shared__ __attribute__((aligned(16))) Sum part[kWaves][kFewRows][kPitch];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int K = A.K, N = A.N;
     const Tile t = find_tile(A, kFewRows, (N + kFewCols - 1) / kFewCols, blockIdx.x);
     if (t.expert < 0) return;
     const int c0 = t.column * kFewCols, row = min(t.begin + (lane & 15), t.end - 1);
-    f32x4 acc[NC] = {};
+    Sum4<T> acc[NC] = {};
     if (t.expert < A.E) {
         int64_t from = row;
         if (GATHERED) {
@@ -519,16 +562,40 @@ __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
     }
 #pragma unroll
     for (int j = 0; j < NC; ++j)
-        *reinterpret_cast<f32x4 *>(&part[wave][lane & 15][j * 16 + (lane >> 4) * 4]) = acc[j];
+        *reinterpret_cast<Sum4<T> *>(&part[wave][lane & 15][j * 16 + (lane >> 4) * 4]) = acc[j];
     __syncthreads();
     const int r = threadIdx.x / (kFewCols / 2), c = threadIdx.x % (kFewCols / 2) * 2;
     if (t.begin + r >= t.end || c0 + c >= N) return;
-    float sum[2] = {};
+    Sum sum[2] = {};
 #pragma unroll
     for (int q = 0; q < kWaves; ++q) sum[0] += part[q][r][c], sum[1] += part[q][r][c + 1];
-    typedef T T2 __attribute__((ext_vector_type(2)));
-    const T2 out = {(T)sum[0], (T)sum[1]};
-    *reinterpret_cast<T2 *>(static_cast<T *>(A.out) + (int64_t)(t.begin + r) * N + c0 + c) = out;
+    if constexpr (kPairs<T>) {
+        int from = t.begin + r;
+        if (GATHERED && t.expert < A.E) from = A.tokens[from];
+        if (from < 0 || (GATHERED && from >= A.T)) from = 0;
+        const int64_t to = (int64_t)(t.begin + r) * N + c0 + c;
+        float y[2] = {};
+        if (t.expert < A.E) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+                if (c0 + c + v < N)
+                    y[v] = (float)sum[v] * A.x_scale[from] * A.w_scale[(int64_t)t.expert * N + c0 + c + v];
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            if (c0 + c + v >= N) break;
+            if (A.out32)
+                A.out32[to + v] = y[v];
+            else if (A.dtype == SK_BF16)
+                static_cast<__bf16 *>(A.out)[to + v] = (__bf16)y[v];
+            else
+                static_cast<_Float16 *>(A.out)[to + v] = (_Float16)y[v];
+        }
+    } else {
+        typedef T T2 __attribute__((ext_vector_type(2)));
+        const T2 out = {(T)sum[0], (T)sum[1]};
+        *reinterpret_cast<T2 *>(static_cast<T *>(A.out) + (int64_t)(t.begin + r) * N + c0 + c) = out;
+    }
 }
 
 // gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here; eight columns to a thread.
@@ -676,6 +743,20 @@ hipError_t launch_few(const ExpertArgs &a, hipStream_t st) {
     });
 }
 
+// Rows in 8 bits, which are whole chunks always.
+template <int TILE, int WM, int WN>
+hipError_t launch_pairs(const ExpertArgs &a, hipStream_t st) {
+    const int64_t tiles = most_row_tiles(a, TILE) * parts_of(a.N, TILE);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(parts_of(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
+        return hipGetLastError();
+    };
+    if (!a.tokens) return go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, false, false, false>);
+    return (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32)
+               ? go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, true, false>)
+               : go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, false, false>);
+}
+
 template <int MODE>
 hipError_t launch_product(const ExpertArgs &a, const Cut &c, hipStream_t st) {
     if (!chunks(a))
@@ -707,6 +788,25 @@ hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, a.N), st);
+}
+
+hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
+    ExpertArgs a = p;
+    a.whole_out = aligned16(a.out) && (int64_t)a.N * (a.dtype == SK_F32 ? 4 : 2) % 16 == 0;
+    a.out32 = a.dtype == SK_F32 ? static_cast<float *>(a.out) : nullptr;
+    const int64_t rows = (int64_t)a.T * a.k;
+    if (rows <= 64 || rows <= 4 * a.E) {
+        const dim3 grid((unsigned)(parts_of(most_row_tiles(a, kFewRows) * parts_of(a.N, kFewCols), 8) * 8));
+        if (a.tokens)
+            hipLaunchKernelGGL((sk_experts_few<Pair, true>), grid, dim3(kThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL((sk_experts_few<Pair, false>), grid, dim3(kThreads), 0, st, a);
+        return hipGetLastError();
+    }
+    const Cut c = cut_rows(a, a.N);
+    if (c.tile == 256) return launch_pairs<256, 2, 4>(a, st);
+    if (c.tile == 128) return launch_pairs<128, 2, 2>(a, st);
+    return launch_pairs<64, 2, 2>(a, st);
 }
 
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
