@@ -15,31 +15,71 @@ namespace {
 
 constexpr int kMostLanes = 1024;
 
+// ---- eight columns ----
+
+template <class T>
+using Raw8 = T __attribute__((ext_vector_type(8)));
+
+// A lane's columns [c, c + 8).  Where a row is no whole number of eights its last window lies back over the one before:
+// the lane's own columns are those from c + lo on, the others are computed and stored twice, with the same bits, and
+// masked in sums.  lo = 8: none.  Rows of less than eight columns have hi of them.
+struct Window {
+    int c, lo, hi;
+    __device__ __forceinline__ Window(int at, int N) {
+        c = max(min(at, N - 8), 0);
+        lo = min(at - c, 8);
+        hi = min(N, 8);
+    }
+    __device__ __forceinline__ bool any() const { return lo < hi; }
+    __device__ __forceinline__ bool own(int i) const { return i >= lo && i < hi; }
+};
+
+template <class T>
+__device__ __forceinline__ Raw8<T> load_raw(const T *p, const Window &w) {
+    Raw8<T> v = {};
+    if (w.hi == 8) {
+        __builtin_memcpy(&v, p + w.c, sizeof(v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < w.hi) v[i] = p[i];
+    }
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void store_window(T *p, const Window &w, const float (&v)[8]) {
+    if (!w.any()) return;
+    if (w.hi == 8)
+        store8(p + w.c, v);
+    else
+        store_some(p, 0, w.hi, v);
+}
 // Eight of a parameter's values, of type T or float.
 template <class T>
-__device__ __forceinline__ void load_param(const void *p, int f32, int64_t at, int left, float (&v)[8]) {
-    if (f32)
-        load_left(static_cast<const float *>(p) + at, left, v);
-    else
-        load_left(static_cast<const T *>(p) + at, left, v);
+__device__ __forceinline__ void load_param(const void *p, int f32, const Window &w, float (&v)[8]) {
+    if (f32) {
+        const Raw8<float> r = load_raw(static_cast<const float *>(p), w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = r[i];
+    } else {
+        const Raw8<T> r = load_raw(static_cast<const T *>(p), w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)r[i];
+    }
 }
+// Of a parameter that may not be there.
 template <class T>
-__device__ __forceinline__ void load_weight(const void *p, int f32, int64_t at, int left, float (&v)[8]) {
+__device__ __forceinline__ void load_param(const void *p, int f32, const Window &w, float none, float (&v)[8]) {
     if (p) {
-        load_param<T>(p, f32, at, left, v);
+        load_param<T>(p, f32, w, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 1.f;
+        for (int i = 0; i < 8; ++i) v[i] = none;
     }
 }
 template <class T>
-__device__ __forceinline__ void load_bias(const void *p, int f32, int64_t at, int left, float (&v)[8]) {
-    if (p) {
-        load_param<T>(p, f32, at, left, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    }
+__device__ __forceinline__ float param_at(const void *p, int f32, int64_t at) {
+    return f32 ? static_cast<const float *>(p)[at] : (float)static_cast<const T *>(p)[at];
 }
 template <class T>
 __device__ __forceinline__ void store_param(void *p, int f32, int64_t at, float v) {
@@ -48,43 +88,51 @@ __device__ __forceinline__ void store_param(void *p, int f32, int64_t at, float 
     else
         static_cast<T *>(p)[at] = (T)v;
 }
-
-// The gate's values for eight columns of a row.
+// The gate of a window of a row.
 template <class T>
-__device__ __forceinline__ void load_gate(const NormArgs &A, int64_t row, int c, int left, float (&v)[8]) {
-    if (A.gate_kind == SK_GATE_COLUMNS) {
-        load_param<T>(A.gate, A.gf32, c, left, v);
-    } else if (A.gate_kind == SK_GATE_FULL) {
-        load_param<T>(A.gate, A.gf32, row * A.N + c, left, v);
+__device__ __forceinline__ void load_gate(const NormArgs &A, int64_t row, const Window &w, float (&v)[8]) {
+    if (A.gate_kind > SK_GATE_ROWS) {
+        const int64_t at = A.gate_kind == SK_GATE_FULL ? row * A.N : 0;
+        const char *p = static_cast<const char *>(A.gate) + at * (A.gf32 ? 4 : (int)sizeof(T));
+        load_param<T>(p, A.gf32, w, v);
     } else {
-        const float one = A.gate_kind == SK_GATE_NONE ? 1.f
-                          : A.gf32                    ? static_cast<const float *>(A.gate)[row]
-                                                      : (float)static_cast<const T *>(A.gate)[row];
+        const float one = A.gate_kind == SK_GATE_NONE ? 1.f : param_at<T>(A.gate, A.gf32, row);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = one;
     }
 }
 
-__device__ __forceinline__ float sum8(const float (&v)[8]) { return tree_sum<8>(v); }
+// A lane's own of eight numbers, added up.
+__device__ __forceinline__ float sum_own(const Window &w, const float (&v)[8]) {
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = w.own(i) ? v[i] : 0.f;
+    return tree_sum<8>(s);
+}
 
 // Each step is rounded by itself, as a program's own steps in 32 bits are: a sum that lies next to a border between two
 // 16-bit numbers then falls to the same side for both.
-__device__ __forceinline__ void norm8_of(const float (&x)[8], float mean, float r, const float (&w)[8],
-                                         const float (&b)[8], float (&y)[8]) {
+template <class T>
+__device__ __forceinline__ void norm8(const Raw8<T> &x, float mean, float r, const float (&w)[8], const float (&b)[8],
+                                      float (&y)[8]) {
 #pragma clang fp contract(off)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float xh = (x[i] - mean) * r;
+        const float xh = ((float)x[i] - mean) * r;
         y[i] = xh * w[i] + b[i];
     }
 }
-__device__ __forceinline__ void sum8_of(float (&y)[8], const float (&gate)[8], const float (&n)[8], float scale) {
+template <class T>
+__device__ __forceinline__ void residual8(const Raw8<T> &residual, float scale, const float (&gate)[8],
+                                          const float (&n)[8], float (&y)[8]) {
 #pragma clang fp contract(off)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = scale * y[i] + gate[i] * n[i];
+    for (int i = 0; i < 8; ++i) y[i] = scale * (float)residual[i] + gate[i] * n[i];
 }
 
-// A row to a group of lanes.  V: the chunks that a lane holds in registers; 0: rows wider than that, read again from
+// ---- forward ----
+
+// A row to a group of lanes.  V: the windows that a lane holds in registers; 0: rows wider than that, read again from
 // the caches for each pass over them.  END: the block's end; else the norm alone, of `residual`.
 template <class T, int V, bool END>
 __global__ __launch_bounds__(kMostLanes) void sk_norm_forward(NormArgs A) {
@@ -96,113 +144,103 @@ __global__ __launch_bounds__(kMostLanes) void sk_norm_forward(NormArgs A) {
     const int N = A.N;
     const float each_n = 1.f / (float)N;
     int turn = 0;
-    // f(chunk held, column, columns left)
+    // f(window held, window)
     auto each = [&](auto f) {
         if constexpr (V > 0) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int c = (v * g.lanes + g.lane) * 8;
-                f(v, c, N - c);
-            }
+            for (int v = 0; v < V; ++v) f(v, Window((v * g.lanes + g.lane) * 8, N));
         } else {
-            for (int c = g.lane * 8; c < N; c += g.lanes * 8) f(0, c, N - c);
+            for (int c = g.lane * 8; c < N; c += g.lanes * 8) f(0, Window(c, N));
         }
     };
-    // Mean and r of a row that `load` puts in x, eight columns at a time.
-    auto statistics = [&](int kind, float eps, float (&x)[H][8], auto load, float &mean, float &r) {
+    // Mean and r of a row that `load` gives a window of.
+    auto statistics = [&](int kind, float eps, auto load, float &mean, float &r) {
         mean = 0.f;
+        float s[1] = {0.f};
         if (kind == SK_NORM_CENTRED) {
-            float s[1] = {};
-            each([&](int v, int c, int left) {
-                if (V == 0) load(v, c, left);
-                s[0] += sum8(x[v]);
+            each([&](int v, const Window &w) {
+                const Raw8<T> x = load(v, w);
+                float q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[i] = (float)x[i];
+                s[0] += sum_own(w, q);
             });
             group_reduce<Sum>(g, s, lds, turn);
             mean = s[0] * each_n;
+            s[0] = 0.f;
         }
-        float s[1] = {};
-        each([&](int v, int c, int left) {
-            if (V == 0) load(v, c, left);
+        each([&](int v, const Window &w) {
+            const Raw8<T> x = load(v, w);
             float q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = i < left ? (x[v][i] - mean) * (x[v][i] - mean) : 0.f;
-            s[0] += sum8(q);
+            for (int i = 0; i < 8; ++i) q[i] = ((float)x[i] - mean) * ((float)x[i] - mean);
+            s[0] += sum_own(w, q);
         });
         group_reduce<Sum>(g, s, lds, turn);
         r = rsqrtf(s[0] * each_n + eps);
     };
-    auto normed = [&](const float (&x)[8], float mean, float r, const void *w, const void *b, int c, int left,
-                      float (&y)[8]) {
-        float wv[8], bv[8];
-        load_weight<T>(w, A.wf32, c, left, wv);
-        load_bias<T>(b, A.wf32, c, left, bv);
-        norm8_of(x, mean, r, wv, bv, y);
-    };
 
     const T *residual = static_cast<const T *>(A.residual) + row * N;
-    float y[H][8];  // the sum, or the norm's input
-    float4 stats = {0.f, 1.f, 0.f, 1.f};
     T *out = static_cast<T *>(A.out) + row * N;
+    Raw8<T> y[H];  // the residual, then the sum; or the norm's input
+    float4 stats = {0.f, 1.f, 0.f, 1.f};
+    if constexpr (V > 0) each([&](int v, const Window &w) { y[v] = load_raw(residual, w); });
     if constexpr (END) {
         const T *h = static_cast<const T *>(A.h) + row * N;
-        float x[H][8];
-        auto load_h = [&](int v, int c, int left) { load_left(h + c, left, x[v]); };
-        if constexpr (V > 0) {
-            each([&](int v, int c, int left) {
-                load_h(v, c, left);
-                load_left(residual + c, left, y[v]);
-            });
-        }
-        if (A.after) statistics(A.after, A.eps_after, x, load_h, stats.x, stats.y);
-        each([&](int v, int c, int left) {
-            if (V == 0) {
-                load_h(v, c, left);
-                load_left(residual + c, left, y[v]);
-            }
-            float n[8], gate[8];
+        Raw8<T> x[H];
+        if constexpr (V > 0) each([&](int v, const Window &w) { x[v] = load_raw(h, w); });
+        auto load_h = [&](int v, const Window &w) { return V > 0 ? x[v] : load_raw(h, w); };
+        if (A.after) statistics(A.after, A.eps_after, load_h, stats.x, stats.y);
+        each([&](int v, const Window &w) {
+            const Raw8<T> hv = load_h(v, w);
+            float n[8], gate[8], wv[8], bv[8], sum[8];
             if (A.after) {
-                normed(x[v], stats.x, stats.y, A.after_w, A.after_b, c, left, n);
+                load_param<T>(A.after_w, A.wf32, w, 1.f, wv);
+                load_param<T>(A.after_b, A.wf32, w, 0.f, bv);
+                norm8<T>(hv, stats.x, stats.y, wv, bv, n);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) n[i] = x[v][i];
+                for (int i = 0; i < 8; ++i) n[i] = (float)hv[i];
             }
-            load_gate<T>(A, row, c, left, gate);
-            sum8_of(y[v], gate, n, A.scale);
+            load_gate<T>(A, row, w, gate);
+            residual8<T>(V > 0 ? y[v] : load_raw(residual, w), A.scale, gate, n, sum);
             // Rounded here: the next norm, and the backward pass of it, take the sum as it is stored.
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[v][i] = i < left ? (float)(T)y[v][i] : 0.f;
-            if (mine) store_left(out + c, left, y[v]);
+            for (int i = 0; i < 8; ++i) y[v][i] = (T)sum[i];
+            if (mine) store_window(out, w, sum);
         });
-    } else if constexpr (V > 0) {
-        each([&](int v, int c, int left) { load_left(residual + c, left, y[v]); });
     }
     if (A.before) {
-        auto load_y = [&](int v, int c, int left) { load_left((END ? out : residual) + c, left, y[v]); };
-        statistics(A.before, A.eps_before, y, load_y, stats.z, stats.w);
-        each([&](int v, int c, int left) {
-            if (V == 0) load_y(v, c, left);
-            float z[8];
-            normed(y[v], stats.z, stats.w, A.before_w, A.before_b, c, left, z);
-            if (mine) store_left(static_cast<T *>(A.next) + row * N + c, left, z);
+        auto load_y = [&](int v, const Window &w) { return V > 0 ? y[v] : load_raw(END ? out : residual, w); };
+        statistics(A.before, A.eps_before, load_y, stats.z, stats.w);
+        each([&](int v, const Window &w) {
+            float z[8], wv[8], bv[8];
+            load_param<T>(A.before_w, A.wf32, w, 1.f, wv);
+            load_param<T>(A.before_b, A.wf32, w, 0.f, bv);
+            norm8<T>(load_y(v, w), stats.z, stats.w, wv, bv, z);
+            if (mine) store_window(static_cast<T *>(A.next) + row * N, w, z);
         });
     }
     if (A.stats && mine && g.lane == 0) reinterpret_cast<float4 *>(A.stats)[row] = stats;
 }
+
+// ---- backward ----
 
 // The sums over the rows.
 enum { kAfterW, kBeforeW, kAfterB, kBeforeB, kGate, kArrays };
 template <int A>
 using Array = std::integral_constant<int, A>;
 
-// A work-group's groups go through rows; the sums over the rows stay in registers (WIDE: in the work-group's own part
-// of memory, and the row is read again from the caches for each pass over it) and are added up over the groups at the
-// end, into one part a work-group.  MORE: there are biases, or a gate that is more than a number a row; without them
-// fewer registers are taken.
+// A work-group's groups go through rows, the next row's loads under way while a row is worked on.  The sums over the
+// rows stay in registers and are added up over the groups at the end, into one part a work-group; WIDE: rows of more
+// windows than lanes, whose sums lie in the work-group's own part of memory and which are read again from the caches for
+// each pass over them.  MORE: there are biases, or a gate that is more than a number a row; without them fewer
+// registers are taken.
 template <class T, bool WIDE, bool END, bool MORE, int THREADS>
-__global__ __launch_bounds__(THREADS) void sk_norm_backward(NormArgs A) {
+__global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_norm_backward(NormArgs A) {
     constexpr int kSums = MORE ? kArrays : kAfterB;
     __shared__ float lds[2][3][kRowWaves];
-    __shared__ __attribute__((aligned(16))) float total[WIDE ? 8 : THREADS * 8];
+    __shared__ float total[WIDE ? 8 : THREADS * 8];
     const RowGroup g(A.lanes);
     const int N = A.N;
     const float each_n = 1.f / (float)N;
@@ -215,158 +253,149 @@ __global__ __launch_bounds__(THREADS) void sk_norm_backward(NormArgs A) {
                                   : A.parts + ((int64_t)blockIdx.x * A.arrays + A.place[array]) * N;
     };
     bool first = true;  // WIDE: the work-group's first row
-    auto add = [&](auto which, int c, int left, const float (&v)[8]) {
+    auto add = [&](auto which, const Window &w, const float (&v)[8]) {
         constexpr int array = decltype(which)::value;
         if constexpr (array >= kSums) {
         } else if constexpr (!WIDE) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) sums[array][i] += v[i];
         } else if (float *to = part_of(array)) {
-            float s[8] = {};
-            if (!first) load_left(to + c, left, s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += v[i];
-            store_left(to + c, left, s);
+            for (int i = 0; i < 8; ++i)
+                if (w.own(i)) to[w.c + i] = first ? v[i] : to[w.c + i] + v[i];
         }
     };
-    float x[8], dy[8], go[8], h[8], gate[8];
-    float wb[8], wa[8], ba[8] = {};
-    auto load_weights = [&](int c, int left) {
-        load_weight<T>(A.before_w, A.wf32, c, left, wb);
-        if (END) {
-            load_weight<T>(A.after_w, A.wf32, c, left, wa);
-            if (MORE) load_bias<T>(A.after_b, A.wf32, c, left, ba);
-        }
+    // A window of a row.
+    struct Row {
+        Raw8<T> x, dy, go, h;
+        float gate[MORE ? 8 : 1];
     };
-    if (!WIDE) load_weights(g.lane * 8, N - g.lane * 8);
-    const int64_t step = (int64_t)gridDim.x * g.groups;
-    for (int64_t r0 = (int64_t)blockIdx.x * g.groups; r0 < A.T; r0 += step) {
+    auto load = [&](int64_t row, const Window &w) {
+        Row v = {};
+        const int64_t at = row * N;
+        if (before) {
+            v.x = load_raw(static_cast<const T *>(A.out) + at, w);
+            v.dy = load_raw(static_cast<const T *>(A.g_next) + at, w);
+        }
+        if (END && A.g_out) v.go = load_raw(static_cast<const T *>(A.g_out) + at, w);
+        if (wants_h) v.h = load_raw(static_cast<const T *>(A.h) + at, w);
+        if constexpr (MORE && END)
+            load_gate<T>(A, row, w, v.gate);
+        else
+            v.gate[0] = !END || A.gate_kind == SK_GATE_NONE ? 1.f : param_at<T>(A.gate, A.gf32, row);
+        return v;
+    };
+    float wb[8], wa[8], ba[8];
+    auto load_weights = [&](const Window &w) {
+        load_param<T>(A.before_w, A.wf32, w, 1.f, wb);
+        if (END) load_param<T>(A.after_w, A.wf32, w, 1.f, wa);
+        if (END) load_param<T>(MORE ? A.after_b : nullptr, A.wf32, w, 0.f, ba);
+    };
+    const Window fixed(g.lane * 8, N);
+    if (!WIDE) load_weights(fixed);
+    const int64_t step = (int64_t)gridDim.x * g.groups, last = A.T - 1;
+    int64_t r0 = (int64_t)blockIdx.x * g.groups;
+    Row v, ahead;
+    float4 stats, stats_ahead;
+    if (!WIDE) ahead = load(min(r0 + g.group, last), fixed);
+    stats_ahead = reinterpret_cast<const float4 *>(A.stats)[min(r0 + g.group, last)];
+    for (; r0 < A.T; r0 += step) {
         const bool mine = r0 + g.group < A.T;
-        const int64_t row = mine ? r0 + g.group : A.T - 1, at = row * N;
-        const float4 stats = reinterpret_cast<const float4 *>(A.stats)[row];
-        auto load = [&](int c, int left) {
-            if (before) {
-                load_left(static_cast<const T *>(A.out) + at + c, left, x);
-                load_left(static_cast<const T *>(A.g_next) + at + c, left, dy);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = dy[i] = 0.f;
-            }
-            if (END && A.g_out) {
-                load_left(static_cast<const T *>(A.g_out) + at + c, left, go);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) go[i] = 0.f;
-            }
-            if (wants_h) load_left(static_cast<const T *>(A.h) + at + c, left, h);
-            if (MORE && END) {
-                load_gate<T>(A, row, c, left, gate);
-            } else {
-                const float one = !END || A.gate_kind == SK_GATE_NONE ? 1.f
-                                  : A.gf32 ? static_cast<const float *>(A.gate)[row]
-                                           : (float)static_cast<const T *>(A.gate)[row];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) gate[i] = one;
-            }
-        };
+        const int64_t row = min(r0 + g.group, last), at = row * N;
+        stats = stats_ahead;
+        if (!WIDE) v = ahead;
+        if (r0 + step < A.T) {
+            const int64_t next = min(r0 + step + g.group, last);
+            if (!WIDE) ahead = load(next, fixed);
+            stats_ahead = reinterpret_cast<const float4 *>(A.stats)[next];
+        }
         auto each = [&](auto f) {
             if constexpr (!WIDE) {
-                f(g.lane * 8, N - g.lane * 8);
+                f(fixed);
             } else {
                 for (int c = g.lane * 8; c < N; c += g.lanes * 8) {
-                    load(c, N - c);
-                    load_weights(c, N - c);
-                    f(c, N - c);
+                    const Window w(c, N);
+                    v = load(row, w);
+                    load_weights(w);
+                    f(w);
                 }
             }
         };
-        if (!WIDE) load(g.lane * 8, N - g.lane * 8);
+        auto gate = [&](int i) { return v.gate[MORE && END ? i : 0]; };
+        auto xh = [&](int i) { return ((float)v.x[i] - stats.z) * stats.w; };
+        auto hh = [&](int i) { return after ? ((float)v.h[i] - stats.x) * stats.y : (float)v.h[i]; };
         float s[2] = {0.f, 0.f};
         if (before) {
-            each([&](int c, int left) {
+            each([&](const Window &w) {
                 float a[8], b[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    a[i] = i < left ? dy[i] * wb[i] : 0.f;
-                    b[i] = a[i] * ((x[i] - stats.z) * stats.w);
+                    a[i] = (float)v.dy[i] * wb[i];
+                    b[i] = a[i] * xh(i);
                 }
-                s[0] += sum8(a), s[1] += sum8(b);
+                s[0] += sum_own(w, a), s[1] += sum_own(w, b);
             });
             group_reduce<Sum>(g, s, lds, turn);
             s[0] = A.before == SK_NORM_CENTRED ? s[0] * each_n : 0.f;
             s[1] *= each_n;
         }
         // The sum's gradient.
-        auto gradient = [&](int left, float (&d)[8]) {
+        auto gradient = [&](float (&d)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                d[i] = go[i];
-                if (before) d[i] += stats.w * (dy[i] * wb[i] - s[0] - (x[i] - stats.z) * stats.w * s[1]);
-                if (i >= left) d[i] = 0.f;
+                d[i] = (float)v.go[i];
+                if (before) d[i] += stats.w * ((float)v.dy[i] * wb[i] - s[0] - xh(i) * s[1]);
             }
         };
         float d[8], q[3] = {0.f, 0.f, 0.f};
-        each([&](int c, int left) {
-            gradient(left, d);
+        each([&](const Window &w) {
+            gradient(d);
             if ((before || WIDE) && mine) {  // WIDE: zeros are written, too
                 float xd[8], yd[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    yd[i] = i < left ? dy[i] : 0.f;
-                    xd[i] = yd[i] * ((x[i] - stats.z) * stats.w);
-                }
-                add(Array<kBeforeW>{}, c, left, xd);
-                add(Array<kBeforeB>{}, c, left, yd);
+                for (int i = 0; i < 8; ++i) yd[i] = (float)v.dy[i], xd[i] = yd[i] * xh(i);
+                add(Array<kBeforeW>{}, w, xd);
+                add(Array<kBeforeB>{}, w, yd);
             }
             if constexpr (!END) {
-                if (mine && A.g_residual) store_left(static_cast<T *>(A.g_residual) + at + c, left, d);
+                if (mine && A.g_residual) store_window(static_cast<T *>(A.g_residual) + at, w, d);
             } else {
-                float n[8], e[8];
+                float e[8];
                 if (mine && A.g_residual) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) e[i] = A.scale * d[i];
-                    store_left(static_cast<T *>(A.g_residual) + at + c, left, e);
+                    store_window(static_cast<T *>(A.g_residual) + at, w, e);
                 }
-                if (wants_h) {
-                    float hh[8];
+                if (A.g_gate) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = d[i] * (after ? hh(i) * wa[i] + ba[i] : hh(i));
+                    if (sums_gate) q[2] += sum_own(w, e);
+                    if (MORE && A.gate_kind == SK_GATE_COLUMNS && mine) add(Array<kGate>{}, w, e);
+                    if (MORE && A.gate_kind == SK_GATE_FULL && mine) {
+                        if (A.gf32)
+                            store_window(static_cast<float *>(A.g_gate) + at, w, e);
+                        else
+                            store_window(static_cast<T *>(A.g_gate) + at, w, e);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= gate(i);
+                if (after) {
+                    float a[8], b[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        hh[i] = after ? (h[i] - stats.x) * stats.y : h[i];
-                        n[i] = after ? hh[i] * wa[i] + ba[i] : h[i];
+                        a[i] = d[i] * wa[i];
+                        b[i] = a[i] * hh(i);
+                        e[i] = d[i] * hh(i);
                     }
-                    if (A.g_gate) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) e[i] = i < left ? d[i] * n[i] : 0.f;
-                        if (sums_gate) q[2] += sum8(e);
-                        if (MORE && A.gate_kind == SK_GATE_COLUMNS && mine) add(Array<kGate>{}, c, left, e);
-                        if (MORE && A.gate_kind == SK_GATE_FULL && mine) {
-                            if (A.gf32)
-                                store_left(static_cast<float *>(A.g_gate) + at + c, left, e);
-                            else
-                                store_left(static_cast<T *>(A.g_gate) + at + c, left, e);
-                        }
+                    q[0] += sum_own(w, a), q[1] += sum_own(w, b);
+                    if (mine) {
+                        add(Array<kAfterW>{}, w, e);
+                        add(Array<kAfterB>{}, w, d);
                     }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = i < left ? d[i] * gate[i] : 0.f;
-                    if (after) {
-                        float a[8], b[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            a[i] = d[i] * wa[i];
-                            b[i] = a[i] * hh[i];
-                            e[i] = d[i] * hh[i];
-                        }
-                        q[0] += sum8(a), q[1] += sum8(b);
-                        if (mine) {
-                            add(Array<kAfterW>{}, c, left, e);
-                            add(Array<kAfterB>{}, c, left, d);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i] = i < left ? d[i] * gate[i] : 0.f;
+                } else if (mine && A.g_h) {
+                    store_window(static_cast<T *>(A.g_h) + at, w, d);
                 }
-                if (!after && mine && A.g_h) store_left(static_cast<T *>(A.g_h) + at + c, left, d);
             }
         });
         if (END && (after || sums_gate)) {
@@ -375,17 +404,16 @@ __global__ __launch_bounds__(THREADS) void sk_norm_backward(NormArgs A) {
             q[1] *= each_n;
             if (sums_gate && mine && g.lane == 0) store_param<T>(A.g_gate, A.gf32, row, q[2]);
             if (after && A.g_h && mine)
-                each([&](int c, int left) {
+                each([&](const Window &w) {
                     if (WIDE) {
-                        gradient(left, d);
+                        gradient(d);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) d[i] *= gate[i];
+                        for (int i = 0; i < 8; ++i) d[i] *= gate(i);
                     }
                     float e[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        e[i] = stats.y * (d[i] * wa[i] - q[0] - (h[i] - stats.x) * stats.y * q[1]);
-                    store_left(static_cast<T *>(A.g_h) + at + c, left, e);
+                    for (int i = 0; i < 8; ++i) e[i] = stats.y * (d[i] * wa[i] - q[0] - hh(i) * q[1]);
+                    store_window(static_cast<T *>(A.g_h) + at, w, e);
                 });
         }
         first = false;
@@ -395,10 +423,11 @@ __global__ __launch_bounds__(THREADS) void sk_norm_backward(NormArgs A) {
         for (int a = 0; a < kSums; ++a) {
             float *to = part_of(a);
             if (!to) continue;
-            // Eight columns a lane, the groups one after the other.
+            // The groups one after the other, by columns.
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) total[threadIdx.x * 8 + i] = sums[a][i];
+            for (int i = 0; i < 8; ++i)
+                if (fixed.own(i)) total[g.group * g.lanes * 8 + fixed.c + i] = sums[a][i];
             __syncthreads();
             for (int c = threadIdx.x; c < N; c += blockDim.x) {
                 float s = 0.f;
@@ -450,24 +479,26 @@ __global__ __launch_bounds__(kSumThreads) void sk_norm_sums(SumArgs A) {
     }
 }
 
-// Rows wider than a work-group's chunks of eight.
-bool wide(int N) { return N > kMostLanes * 8; }
-
 // Threads and work-groups of the backward pass.
+bool wide(int N) { return N > kMostLanes * 8; }
 int backward_threads(int lanes) { return lanes <= 512 ? 512 : 1024; }
-int backward_blocks(int T, int N) {
+// more: as the kernel's; it has twice the registers, so that one work-group of 512 threads fits on a CU instead of two.
+int backward_blocks(int T, int N, bool more) {
     const int lanes = row_lanes(N, kMostLanes), groups = backward_threads(lanes) / lanes;
-    const int64_t most = (1 << 22) / N < 128 ? 128 : (1 << 22) / N > 512 ? 512 : (1 << 22) / N;
+    const int64_t most = lanes <= 512 && !more ? 512 : 256;
     const int64_t all = ((int64_t)T + groups - 1) / groups;
     return (int)(all < most ? all : most);
 }
 
 }  // namespace
 
-size_t norm_workspace_bytes(int T, int N) { return (size_t)backward_blocks(T, N) * kArrays * N * 4; }
+size_t norm_workspace_bytes(int T, int N) { return (size_t)backward_blocks(T, N, false) * kArrays * N * 4; }
 
 hipError_t launch_norm_forward(NormArgs a, hipStream_t st) {
+    // A window a lane as long as there are lanes: four to a lane and a quarter of the lanes took 190 against 173 us for
+    // the end of a block of 65536 x 2048, 6.8 against 3.8 us for 4 x 2048.
     a.lanes = row_lanes(a.N, kMostLanes);
+    const int windows = (a.N + a.lanes * 8 - 1) / (a.lanes * 8), V = windows <= 2 ? windows : windows <= 4 ? 4 : 0;
     const int threads = a.lanes < 256 ? 256 : a.lanes, groups = threads / a.lanes;
     const dim3 grid((unsigned)(((int64_t)a.T + groups - 1) / groups));
     return with_type(a.dtype, [&](auto type) {
@@ -476,8 +507,14 @@ hipError_t launch_norm_forward(NormArgs a, hipStream_t st) {
             hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
             return hipGetLastError();
         };
-        if (a.end) return wide(a.N) ? go(sk_norm_forward<T, 0, true>) : go(sk_norm_forward<T, 1, true>);
-        return wide(a.N) ? go(sk_norm_forward<T, 0, false>) : go(sk_norm_forward<T, 1, false>);
+        auto by_end = [&](auto windows) {
+            constexpr int W = decltype(windows)::value;
+            return a.end ? go(sk_norm_forward<T, W, true>) : go(sk_norm_forward<T, W, false>);
+        };
+        if (V == 1) return by_end(std::integral_constant<int, 1>{});
+        if (V == 2) return by_end(std::integral_constant<int, 2>{});
+        if (V == 4) return by_end(std::integral_constant<int, 4>{});
+        return by_end(std::integral_constant<int, 0>{});
     });
 }
 
@@ -496,7 +533,7 @@ hipError_t launch_norm_backward(NormArgs a, void *ws, hipStream_t st) {
     }
     const bool more = a.gate_kind > SK_GATE_ROWS || a.after_b || a.g_after_b || a.g_before_b;
     s.parts = a.parts;
-    s.blocks = backward_blocks(a.T, a.N);
+    s.blocks = backward_blocks(a.T, a.N, more);
     s.arrays = a.arrays;
     s.N = a.N;
     const int threads = backward_threads(a.lanes);

@@ -203,7 +203,8 @@ def sinkhorn_residual_norm_forward(h, residual, gate=None, scale=1.0, after=None
 @_on_stream
 def sinkhorn_residual_norm_backward(h, out, stats, grad_out=None, grad_next=None, gate=None, scale=1.0, after=None,
                                     before=None, workspace=None):
-    """NormGradients from those of out and next (each may be None)."""
+    """NormGradients from those of out and next (each may be None); those of h and residual are one tensor where out is
+    their plain sum."""
     sizes = _residual_sizes(h, gate, scale, after, before)
     _match(out, "out", h, h.shape, h.dtype)
     _match(stats, "stats", h, (sizes[0], 4), torch.float32)
@@ -220,11 +221,17 @@ def _run_residual_backward(h, out, gate, after, before, stats, g_out, g_next, si
     rows = next(t for t in (h, out, g_out) if t is not None)
     like = (rows, rows, gate, _of(after, "weight"), _of(after, "bias"), _of(before, "weight"), _of(before, "bias"))
     grads = [torch.empty_like(t) if w else None for t, w in zip(like, wanted)]
+    # Where out = residual + h both have one gradient: it is written once, and is one tensor for both, as of a sum.
+    same = after is None and gate is None and sizes[8] == 1.0 and wanted[0] and wanted[1]
+    if same:
+        grads[0] = None
     sums = any(wanted[3:]) or (wanted[2] and sizes[4] == _COLUMNS)
     scratch = _workspace(workspace, need, stats.device) if sums else None
     _call(load_library().sinkhorn_residual_norm_backward, stats.device, ref, _ptr(h), _ptr(out), _ptr(gate),
           _ptr(_of(after, "weight")), _ptr(_of(after, "bias")), _ptr(_of(before, "weight")), stats.data_ptr(),
           _ptr(g_out), _ptr(g_next), *(_ptr(g) for g in grads), _ptr(scratch), need)
+    if same:
+        grads[0] = grads[1]
     return NormGradients(*grads)
 
 

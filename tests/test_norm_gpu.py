@@ -356,3 +356,27 @@ def test_wrong_arguments():
                         (lambda: sk.sinkhorn_residual_norm(x, x, after=sk.Norm(w.cpu())), TypeError)):
         with pytest.raises(error):
             call()
+
+
+def test_a_plain_sum_has_one_gradient_for_both():
+    """out = residual + h: the gradients are equal, whichever are asked for; with a scale they are not."""
+    T, N = 70, 96
+    h, residual, w = rows(T, N, 1, BF16), rows(T, N, 2, BF16), make(N, seed=3, plus=1.0, dtype=BF16).requires_grad_()
+    g = make(T, N, seed=4, dtype=BF16)
+
+    def grads(need, scale=1.0):
+        a, b = h.clone().requires_grad_(need[0]), residual.clone().requires_grad_(need[1])
+        y = sk.sinkhorn_residual_norm(a, b, scale=scale, before=sk.Norm(w))
+        return torch.autograd.grad(y, [t for t in (a, b) if t.requires_grad], (g, g))
+    both = grads((True, True))
+    assert torch.equal(*both)
+    assert torch.equal(grads((True, False))[0], both[0]) and torch.equal(grads((False, True))[0], both[0])
+    a, b = grads((True, True), 0.5)
+    assert torch.equal((0.5 * a.float()).to(BF16), b)
+    x = h.clone().requires_grad_()  # accumulated in place, the two do not disturb each other
+    y = residual.clone().requires_grad_()
+    for _ in range(2):
+        o, n = sk.sinkhorn_residual_norm(x, y, before=sk.Norm(w.detach()))
+        torch.autograd.backward((o, n), (g, g))
+    want = (2 * both[0].float()).to(BF16)
+    assert torch.equal(x.grad, want) and torch.equal(y.grad, want)
