@@ -62,18 +62,27 @@ __device__ __forceinline__ int xcd_order(int b, int tiles) {
 struct Tile {
     int expert, begin, end, column;
 };
+// The inclusive sum over the wavefront's lanes.
+__device__ __forceinline__ int lane_sums(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);   // row_shr:2
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);   // row_shr:4
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);   // row_shr:8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 to rows 2 and 3
+    return v;
+}
 __device__ __forceinline__ Tile find_tile(const ExpertArgs &A, int tile, int columns, int b) {
     const int lane = threadIdx.x & 63;
     const auto row_tiles = [&](RowRange r) { return (r.end - r.begin + tile - 1) / tile; };
     const RowRange none = expert_rows(A, A.E);
-    int in_experts = 0;
-    for (int e0 = 0; e0 < A.E; e0 += 64) {
-        int n = e0 + lane < A.E ? row_tiles(expert_rows(A, e0 + lane)) : 0;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d, 64);
-        in_experts += n;
-    }
-    in_experts = __builtin_amdgcn_readfirstlane(in_experts);
+    // The first 64 experts' ranges and sums stay at hand.
+    RowRange mine = {0, 0};
+    if (lane < A.E) mine = expert_rows(A, lane);
+    int n = row_tiles(mine), upto = lane_sums(n);
+    int in_experts = __builtin_amdgcn_readlane(upto, 63);
+    for (int e0 = 64; e0 < A.E; e0 += 64)
+        in_experts += __builtin_amdgcn_readlane(lane_sums(e0 + lane < A.E ? row_tiles(expert_rows(A, e0 + lane)) : 0), 63);
     const int t = xcd_order(b, (in_experts + row_tiles(none)) * columns);
     if (t < 0) return {-1, 0, 0, 0};
     const int row = t / columns;
@@ -81,17 +90,7 @@ __device__ __forceinline__ Tile find_tile(const ExpertArgs &A, int tile, int col
     int expert = A.E, before = in_experts;
     if (row < in_experts) {
         before = 0;
-        for (int e0 = 0; e0 < A.E; e0 += 64) {
-            RowRange mine = {0, 0};
-            if (e0 + lane < A.E) mine = expert_rows(A, e0 + lane);
-            const int n = row_tiles(mine);
-            int upto = n;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int up = __shfl_up(upto, d, 64);
-                if (lane >= d) upto += up;
-            }
-            upto += before;
+        for (int e0 = 0;;) {
             const uint64_t who = __builtin_amdgcn_ballot_w64(row < upto && row >= upto - n);
             if (who) {
                 const int q = __builtin_ctzll(who);
@@ -102,12 +101,17 @@ __device__ __forceinline__ Tile find_tile(const ExpertArgs &A, int tile, int col
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
+            e0 += 64;
+            if (e0 >= A.E) return {-1, 0, 0, 0};
+            mine = {0, 0};
+            if (e0 + lane < A.E) mine = expert_rows(A, e0 + lane);
+            n = row_tiles(mine);
+            upto = lane_sums(n) + before;
         }
-        if (expert == A.E) return {-1, 0, 0, 0};
     }
-    const int i = t - before * columns, n = row_tiles(r);
+    const int i = t - before * columns, m = row_tiles(r);
     const int group = i / (4 * columns), j = i - group * 4 * columns;
-    const int high = min(4, n - group * 4);
+    const int high = min(4, m - group * 4);
     const int begin = r.begin + (group * 4 + j % high) * tile;
     return {expert, begin, min(begin + tile, r.end), j / high};
 }

@@ -184,6 +184,8 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     static_assert(BM / WM * (BN * 4 + 32) <= kOut);
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStep > kOut ? 2 * kStep : kOut];
 
+    __shared__ __attribute__((aligned(16))) float scales[kPairs<T> ? BM + BN : 1];  // of the tile's rows and columns
+
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int K = A.K, N = A.N, cols = MODE == kForward ? N : K;
     const T *x = static_cast<const T *>(A.x), *w = static_cast<const T *>(A.w), *gy = static_cast<const T *>(A.gy);
@@ -218,6 +220,20 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     m1 = __builtin_amdgcn_readfirstlane(m1), c0 = __builtin_amdgcn_readfirstlane(c0);
     r0 = __builtin_amdgcn_readfirstlane(r0), deep = __builtin_amdgcn_readfirstlane(deep);
 
+    // A scale a thread, under way with the first copies.
+    [[maybe_unused]] float scale = 0.f;
+    if constexpr (kPairs<T>) {
+        static_assert(BM + BN <= WM * WN * 64);
+        const int i = threadIdx.x;
+        if (deep > 0 && i < BM) {
+            const int r = min(m0 + i, m1 - 1);
+            int t = GATHERED ? A.tokens[r] : r;
+            if (GATHERED && (t < 0 || t >= A.T)) t = 0;
+            scale = A.x_scale[t];
+        } else if (deep > 0 && i < BM + BN) {
+            scale = A.w_scale[(int64_t)e * N + min(c0 + i - BM, N - 1)];
+        }
+    }
     Sum4<T> acc[FM][FN] = {};
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     const bool idle = m0 + wm >= m1 || c0 + wn >= cols;  // the wavefront's part lies past the edge: it copies only
@@ -428,24 +444,21 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     // The results go through LDS, so that whole lines are written: a lane holds four neighbouring columns of a row (row
     // lane % 16, columns (lane / 16) * 4 of a 16 x 16 block), 32 bytes a row of a block.  Written straight from there the
     // products took 6 % longer.  Results in 32 bits go in WM passes, of BM / WM rows.
+    if constexpr (kPairs<T>) {
+        if (threadIdx.x < BM + BN) scales[threadIdx.x] = scale;
+    }
     __syncthreads();  // nobody reads the last step's operands any more
     [[maybe_unused]] float x_scale[kPairs<T> ? FM : 1], w_scale[kPairs<T> ? FN : 1][4];
     if constexpr (kPairs<T>) {
         static_assert(MODE == kForward && !STAGED);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int r = min(m0 + wm + i * 16 + (lane & 15), m1 - 1);
-            int t = GATHERED ? A.tokens[r] : r;
-            if (GATHERED && (t < 0 || t >= A.T)) t = 0;
-            x_scale[i] = deep > 0 ? A.x_scale[t] : 0.f;
+        for (int i = 0; i < FM; ++i) x_scale[i] = scales[wm + i * 16 + (lane & 15)];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const f32x4 w4 = *reinterpret_cast<const f32x4 *>(&scales[BM + wn + j * 16 + (lane >> 4) * 4]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) w_scale[j][v] = w4[v];
         }
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int c = min(c0 + wn + j * 16 + (lane >> 4) * 4 + v, N - 1);
-                w_scale[j][v] = deep > 0 ? A.w_scale[(int64_t)e * N + c] : 0.f;
-            }
     }
     // Whether results are stored in whole 16 bytes: rows in 8 bits are, whatever the results' columns.
     const bool whole_out = !STAGED && (!kPairs<T> || A.whole_out);

@@ -23,41 +23,50 @@ constexpr int kBlockLanes = kPackBlock / 8;  // lanes of a block of columns
 // The scale of numbers up to `most`.  Where it is so small that its reciprocal would overflow, numbers and scale are
 // multiplied by a power of two first (exactly).
 struct Scale {
-    float s, up, scaled, inverse;
+    float s, scaled, inverse;
+    bool tiny;
 };
+constexpr float kUp = 0x1p64f;
 __device__ __forceinline__ Scale scale_of(float most) {
     Scale c;
     c.s = most / 127.f;
     if (!(most < __builtin_inff())) c.s = __builtin_nanf("");
-    c.up = most < 0x1p-96f ? 0x1p64f : 1.f;
-    c.scaled = c.s * c.up;
+    c.tiny = most < 0x1p-96f;
+    c.scaled = c.tiny ? c.s * kUp : c.s;
     c.inverse = c.scaled > 0.f ? __builtin_amdgcn_rcpf(c.scaled) : 0.f;  // NaN and 0: 0
     return c;
 }
 
-// Eight whole numbers x / s, to nearest even of the exact quotient, as bytes.  The quotient by the reciprocal is off by
-// less than 2^-15, so it rounds as the exact one does unless it lies that near to a half.  There the remainder x - q s
-// decides, which a fused multiplication and addition gives exactly (it is a multiple of the last place of s or of x, and
-// no larger than s).  Added to 1.5 2^23, a number has its whole part in its lowest bits.
+// Eight whole numbers x / s, to nearest even of the exact quotient, as bytes.  Added to 1.5 2^23, a number has its whole
+// part in its lowest bits.  The quotient by the reciprocal is off by less than 2^-15, so it rounds as the exact one does
+// unless it lies that near to a half.  There the remainder x - q s decides, which a fused multiplication and addition
+// gives exactly (it is a multiple of the last place of s or of x, and no larger than s).
 struct Bytes8 {
     uint32_t w[2];
 };
 __device__ __forceinline__ Bytes8 round8(const float (&x)[8], const Scale &c) {
     constexpr float kMagic = 12582912.f;
-    float v[8], q[8], far = 0.f;
+    float v[8], f[8], far = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[i];
+    if (c.tiny) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= kUp;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        v[i] = x[i] * c.up;
-        q[i] = fmaf(v[i], c.inverse, kMagic) - kMagic;
-        far = fmaxf(far, fabsf(fmaf(v[i], c.inverse, -q[i])));
+        f[i] = fmaf(v[i], c.inverse, kMagic);
+        far = fmaxf(far, fabsf(fmaf(v[i], c.inverse, kMagic - f[i])));
     }
-    if (far > 0.5f - 0x1p-14f) {
+    if (c.tiny || far > 0.5f - 0x1p-14f) {
         const uint32_t half = __float_as_uint(0.5f * c.scaled);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float left = fmaf(-q[i], c.scaled, v[i]);
+            float q = f[i] - kMagic;
+            const float left = fmaf(-q, c.scaled, v[i]);
             // above a half, or a half away from an odd number
-            if (__float_as_uint(fabsf(left)) + ((uint32_t)(int)q[i] & 1) > half) q[i] += left < 0.f ? -1.f : 1.f;
+            if (__float_as_uint(fabsf(left)) + ((uint32_t)(int)q & 1) > half) q += left < 0.f ? -1.f : 1.f;
+            f[i] = __builtin_amdgcn_fmed3f(q, -127.f, 127.f) + kMagic;  // a scale of few bits: past 127
         }
     }
     Bytes8 b;
@@ -65,13 +74,9 @@ __device__ __forceinline__ Bytes8 round8(const float (&x)[8], const Scale &c) {
     for (int h = 0; h < 2; ++h) {
         uint32_t u[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float k = __builtin_amdgcn_fmed3f(q[h * 4 + i], -127.f, 127.f);  // a scale of few bits: past 127
-            u[i] = __float_as_uint(k + kMagic);
-        }
-        const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400);
-        b.w[h] = lo | hi << 16;
-        if (!(c.inverse > 0.f)) b.w[h] = 0;  // infinities and NaN under a scale of NaN, too
+        for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(f[h * 4 + i]);
+        const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0c);
+        b.w[h] = c.inverse > 0.f ? lo | hi : 0;  // infinities and NaN under a scale of NaN: 0, too
     }
     return b;
 }
