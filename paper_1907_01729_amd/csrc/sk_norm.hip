@@ -234,11 +234,13 @@ using Array = std::integral_constant<int, A>;
 // A work-group's groups go through rows, the next row's loads under way while a row is worked on.  The sums over the
 // rows stay in registers and are added up over the groups at the end, into one part a work-group; WIDE: rows of more
 // windows than lanes, whose sums lie in the work-group's own part of memory and which are read again from the caches for
-// each pass over them.  MORE: there are biases, or a gate that is more than a number a row; without them fewer
-// registers are taken.
-template <class T, bool WIDE, bool END, bool MORE, int THREADS>
-__global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_norm_backward(NormArgs A) {
-    constexpr int kSums = MORE ? kArrays : kAfterB;
+// each pass over them.  BIAS: there are sums for biases; GATE: the gate is more than a number a row.  Without them fewer
+// registers are taken: two work-groups of 512 threads fit on a CU with up to 128 (16-bit rows, no such gate).  Of 1024
+// threads one does; where its registers do not hold the next row, too, that is loaded when it is its turn.
+template <class T, bool WIDE, bool END, bool BIAS, bool GATE, int THREADS>
+__global__ __launch_bounds__(THREADS, GATE || (END && sizeof(T) == 4) ? 2 : 4) void sk_norm_backward(NormArgs A) {
+    constexpr bool kAhead = !WIDE && (THREADS < 1024 || !END || (sizeof(T) == 2 && !BIAS && !GATE));
+    constexpr auto has = [](int array) { return array < kAfterB || (array == kGate ? GATE : BIAS); };
     __shared__ float lds[2][3][kRowWaves];
     __shared__ float total[WIDE ? 8 : THREADS * 8];
     const RowGroup g(A.lanes);
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
     const bool before = A.before && A.g_next, after = END && A.after;
     const bool wants_h = after || (END && A.g_gate), sums_gate = END && A.gate_kind == SK_GATE_ROWS && A.g_gate;
     int turn = 0;
-    float sums[WIDE ? 1 : kSums][8] = {};
+    float sums[WIDE ? 1 : kArrays][8] = {};
     auto part_of = [&](int array) {
         return A.place[array] < 0 ? nullptr
                                   : A.parts + ((int64_t)blockIdx.x * A.arrays + A.place[array]) * N;
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
     bool first = true;  // WIDE: the work-group's first row
     auto add = [&](auto which, const Window &w, const float (&v)[8]) {
         constexpr int array = decltype(which)::value;
-        if constexpr (array >= kSums) {
+        if constexpr (!has(array)) {
         } else if constexpr (!WIDE) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) sums[array][i] += v[i];
@@ -267,8 +269,8 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
     };
     // A window of a row.
     struct Row {
-        Raw8<T> x, dy, go, h;
-        float gate[MORE ? 8 : 1];
+        Raw8<T> x, dy, go, h, gate;
+        float one;  // the gate, where it is a number
     };
     auto load = [&](int64_t row, const Window &w) {
         Row v = {};
@@ -279,17 +281,16 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
         }
         if (END && A.g_out) v.go = load_raw(static_cast<const T *>(A.g_out) + at, w);
         if (wants_h) v.h = load_raw(static_cast<const T *>(A.h) + at, w);
-        if constexpr (MORE && END)
-            load_gate<T>(A, row, w, v.gate);
-        else
-            v.gate[0] = !END || A.gate_kind == SK_GATE_NONE ? 1.f : param_at<T>(A.gate, A.gf32, row);
+        if constexpr (GATE) {
+            if (A.gate_kind == SK_GATE_FULL && !A.gf32) v.gate = load_raw(static_cast<const T *>(A.gate) + at, w);
+        }
+        v.one = !END || A.gate_kind != SK_GATE_ROWS ? 1.f : param_at<T>(A.gate, A.gf32, row);
         return v;
     };
-    float wb[8], wa[8], ba[8];
+    float wb[8], wa[8];
     auto load_weights = [&](const Window &w) {
         load_param<T>(A.before_w, A.wf32, w, 1.f, wb);
         if (END) load_param<T>(A.after_w, A.wf32, w, 1.f, wa);
-        if (END) load_param<T>(MORE ? A.after_b : nullptr, A.wf32, w, 0.f, ba);
     };
     const Window fixed(g.lane * 8, N);
     if (!WIDE) load_weights(fixed);
@@ -297,16 +298,19 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
     int64_t r0 = (int64_t)blockIdx.x * g.groups;
     Row v, ahead;
     float4 stats, stats_ahead;
-    if (!WIDE) ahead = load(min(r0 + g.group, last), fixed);
+    if (kAhead) ahead = load(min(r0 + g.group, last), fixed);
     stats_ahead = reinterpret_cast<const float4 *>(A.stats)[min(r0 + g.group, last)];
     for (; r0 < A.T; r0 += step) {
         const bool mine = r0 + g.group < A.T;
         const int64_t row = min(r0 + g.group, last), at = row * N;
         stats = stats_ahead;
-        if (!WIDE) v = ahead;
+        if (kAhead)
+            v = ahead;
+        else if (!WIDE)
+            v = load(row, fixed);
         if (r0 + step < A.T) {
             const int64_t next = min(r0 + step + g.group, last);
-            if (!WIDE) ahead = load(next, fixed);
+            if (kAhead) ahead = load(next, fixed);
             stats_ahead = reinterpret_cast<const float4 *>(A.stats)[next];
         }
         auto each = [&](auto f) {
@@ -321,7 +325,18 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
                 }
             }
         };
-        auto gate = [&](int i) { return v.gate[MORE && END ? i : 0]; };
+        // d times the gate.
+        auto gated = [&](const Window &w, float (&d)[8]) {
+            if (GATE && (A.gate_kind == SK_GATE_COLUMNS || (A.gate_kind == SK_GATE_FULL && A.gf32))) {
+                float gate[8];
+                load_gate<T>(A, row, w, gate);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= gate[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= GATE && A.gate_kind == SK_GATE_FULL ? (float)v.gate[i] : v.one;
+            }
+        };
         auto xh = [&](int i) { return ((float)v.x[i] - stats.z) * stats.w; };
         auto hh = [&](int i) { return after ? ((float)v.h[i] - stats.x) * stats.y : (float)v.h[i]; };
         float s[2] = {0.f, 0.f};
@@ -367,19 +382,20 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
                     store_window(static_cast<T *>(A.g_residual) + at, w, e);
                 }
                 if (A.g_gate) {
+                    float ba[8];
+                    load_param<T>(A.after_b, A.wf32, w, 0.f, ba);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) e[i] = d[i] * (after ? hh(i) * wa[i] + ba[i] : hh(i));
                     if (sums_gate) q[2] += sum_own(w, e);
-                    if (MORE && A.gate_kind == SK_GATE_COLUMNS && mine) add(Array<kGate>{}, w, e);
-                    if (MORE && A.gate_kind == SK_GATE_FULL && mine) {
+                    if (GATE && A.gate_kind == SK_GATE_COLUMNS && mine) add(Array<kGate>{}, w, e);
+                    if (GATE && A.gate_kind == SK_GATE_FULL && mine) {
                         if (A.gf32)
                             store_window(static_cast<float *>(A.g_gate) + at, w, e);
                         else
                             store_window(static_cast<T *>(A.g_gate) + at, w, e);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= gate(i);
+                gated(w, d);
                 if (after) {
                     float a[8], b[8];
 #pragma unroll
@@ -407,8 +423,7 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
                 each([&](const Window &w) {
                     if (WIDE) {
                         gradient(d);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) d[i] *= gate(i);
+                        gated(w, d);
                     }
                     float e[8];
 #pragma unroll
@@ -420,8 +435,8 @@ __global__ __launch_bounds__(THREADS, MORE || sizeof(T) == 4 ? 2 : 4) void sk_no
     }
     if constexpr (!WIDE) {
 #pragma unroll
-        for (int a = 0; a < kSums; ++a) {
-            float *to = part_of(a);
+        for (int a = 0; a < kArrays; ++a) {
+            float *to = has(a) ? part_of(a) : nullptr;
             if (!to) continue;
             // The groups one after the other, by columns.
             __syncthreads();
@@ -482,10 +497,10 @@ __global__ __launch_bounds__(kSumThreads) void sk_norm_sums(SumArgs A) {
 // Threads and work-groups of the backward pass.
 bool wide(int N) { return N > kMostLanes * 8; }
 int backward_threads(int lanes) { return lanes <= 512 ? 512 : 1024; }
-// more: as the kernel's; it has twice the registers, so that one work-group of 512 threads fits on a CU instead of two.
-int backward_blocks(int T, int N, bool more) {
+// few: as many as fit on the CUs one by one.
+int backward_blocks(int T, int N, bool few) {
     const int lanes = row_lanes(N, kMostLanes), groups = backward_threads(lanes) / lanes;
-    const int64_t most = lanes <= 512 && !more ? 512 : 256;
+    const int64_t most = lanes <= 512 && !few ? 512 : 256;
     const int64_t all = ((int64_t)T + groups - 1) / groups;
     return (int)(all < most ? all : most);
 }
@@ -495,9 +510,11 @@ int backward_blocks(int T, int N, bool more) {
 size_t norm_workspace_bytes(int T, int N) { return (size_t)backward_blocks(T, N, false) * kArrays * N * 4; }
 
 hipError_t launch_norm_forward(NormArgs a, hipStream_t st) {
-    // A window a lane as long as there are lanes: four to a lane and a quarter of the lanes took 190 against 173 us for
-    // the end of a block of 65536 x 2048, 6.8 against 3.8 us for 4 x 2048.
-    a.lanes = row_lanes(a.N, kMostLanes);
+    // Two windows a lane, which wait for memory together: the norm of 65536 x 2048 in 95 us, with one 110; a block's end
+    // with two norms, 16384 x 2048, in 47, with one 54.  A block's end loads two arrays at once already: with one norm
+    // or none 181 us with a window, 191 with two.
+    const bool two = !a.end || (a.after && a.before);
+    a.lanes = row_lanes(two ? (a.N + 1) / 2 : a.N, kMostLanes);
     const int windows = (a.N + a.lanes * 8 - 1) / (a.lanes * 8), V = windows <= 2 ? windows : windows <= 4 ? 4 : 0;
     const int threads = a.lanes < 256 ? 256 : a.lanes, groups = threads / a.lanes;
     const dim3 grid((unsigned)(((int64_t)a.T + groups - 1) / groups));
@@ -531,9 +548,9 @@ hipError_t launch_norm_backward(NormArgs a, void *ws, hipStream_t st) {
         s.f32[a.arrays] = i == kGate ? a.gf32 : a.wf32;
         a.place[i] = a.arrays++;
     }
-    const bool more = a.gate_kind > SK_GATE_ROWS || a.after_b || a.g_after_b || a.g_before_b;
+    const bool bias = a.g_after_b || a.g_before_b, gate = a.gate_kind > SK_GATE_ROWS;
     s.parts = a.parts;
-    s.blocks = backward_blocks(a.T, a.N, more);
+    s.blocks = backward_blocks(a.T, a.N, gate || (a.end && a.dtype == SK_F32));
     s.arrays = a.arrays;
     s.N = a.N;
     const int threads = backward_threads(a.lanes);
@@ -543,16 +560,22 @@ hipError_t launch_norm_backward(NormArgs a, void *ws, hipStream_t st) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks), dim3(threads), 0, st, a);
             return hipGetLastError();
         };
-        auto by_more = [&](auto is_wide, auto end, auto most) {
+        auto by_sums = [&](auto is_wide, auto end, auto most) {
             constexpr bool W = decltype(is_wide)::value, B = decltype(end)::value;
             constexpr int M = decltype(most)::value;
-            return more ? go(sk_norm_backward<T, W, B, true, M>) : go(sk_norm_backward<T, W, B, false, M>);
+            if constexpr (B) {
+                if (gate)
+                    return bias ? go(sk_norm_backward<T, W, B, true, true, M>)
+                                : go(sk_norm_backward<T, W, B, false, true, M>);
+            }
+            return bias ? go(sk_norm_backward<T, W, B, true, false, M>)
+                        : go(sk_norm_backward<T, W, B, false, false, M>);
         };
         auto by_size = [&](auto end) {
             constexpr std::integral_constant<int, 512> half{};
             constexpr std::integral_constant<int, 1024> full{};
-            if (wide(a.N)) return by_more(std::true_type{}, end, full);
-            return threads == 512 ? by_more(std::false_type{}, end, half) : by_more(std::false_type{}, end, full);
+            if (wide(a.N)) return by_sums(std::true_type{}, end, full);
+            return threads == 512 ? by_sums(std::false_type{}, end, half) : by_sums(std::false_type{}, end, full);
         };
         const hipError_t e = a.T == 0 ? hipSuccess : a.end ? by_size(std::true_type{}) : by_size(std::false_type{});
         if (e != hipSuccess || !a.arrays) return e;
