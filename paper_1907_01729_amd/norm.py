@@ -58,23 +58,29 @@ def _kind(norm):
     return 0 if norm is None else 2 if norm.center else 1
 
 
-def _parameters(x, **norms):
-    """Checks the norms' weights and biases and gives their common type."""
+def _parameter(t, name, x, N, found):
+    """Checks a weight or bias; gives its type, which is the type of all of them."""
+    _typed(t, name)
+    _match(t, name, x)
+    if t.dim() != 1 or t.shape[0] != N:
+        raise ValueError(f"{name} must be [{N}], got {list(t.shape)}")
+    if t.dtype != x.dtype and t.dtype != torch.float32:
+        raise TypeError(f"{name} must be {x.dtype} or float32, got {t.dtype}")
+    if found is not None and t.dtype != found:
+        raise TypeError(f"all weights and biases must have one type, got {found} and {t.dtype}")
+    return t.dtype
+
+
+def _parameters(x, N, *norms):
+    """Checks the named norms' weights and biases and gives their type."""
     found = None
-    for name, norm in norms.items():
+    for name, norm in norms:
         if norm is None:
             continue
-        for what in ("weight", "bias"):
-            t = getattr(norm, what)
-            if t is None:
-                continue
-            _typed(t, f"{name}.{what}")
-            _match(t, f"{name}.{what}", x, (x.shape[1],))
-            if t.dtype != x.dtype and t.dtype != torch.float32:
-                raise TypeError(f"{name}.{what} must be {x.dtype} or float32, got {t.dtype}")
-            if found is not None and t.dtype != found:
-                raise TypeError(f"all weights and biases must have one type, got {found} and {t.dtype}")
-            found = t.dtype
+        if norm.weight is not None:
+            found = _parameter(norm.weight, name + ".weight", x, N, found)
+        if norm.bias is not None:
+            found = _parameter(norm.bias, name + ".bias", x, N, found)
     return _DTYPE[x.dtype if found is None else found]
 
 
@@ -94,7 +100,10 @@ def _gate(gate, x):
 
 
 def _as_contiguous(norm):
-    return None if norm is None else norm._replace(weight=_contiguous(norm.weight), bias=_contiguous(norm.bias))
+    if norm is None or ((norm.weight is None or norm.weight.is_contiguous()) and
+                        (norm.bias is None or norm.bias.is_contiguous())):
+        return norm
+    return norm._replace(weight=_contiguous(norm.weight), bias=_contiguous(norm.bias))
 
 
 def _of(norm, what):
@@ -106,7 +115,7 @@ def _of(norm, what):
 def _norm_sizes(x, norm):
     T, N = _rows(x, "x")
     dtype = _DTYPE[x.dtype]
-    return T, N, dtype, _parameters(x, norm=norm), 0, 0, 0, _kind(norm), 1.0, 0.0, float(norm.eps)
+    return T, N, dtype, _parameters(x, N, ("norm", norm)), 0, 0, 0, _kind(norm), 1.0, 0.0, float(norm.eps)
 
 
 def _run_norm(x, norm, sizes, with_stats):
@@ -177,7 +186,7 @@ def sinkhorn_norm(x, norm=Norm()):
 def _residual_sizes(h, gate, scale, after, before):
     T, N = _rows(h, "h")
     kind, gdtype = _gate(gate, h)
-    return (T, N, _DTYPE[h.dtype], _parameters(h, after=after, before=before), kind, gdtype, _kind(after),
+    return (T, N, _DTYPE[h.dtype], _parameters(h, N, ("after", after), ("before", before)), kind, gdtype, _kind(after),
             _kind(before), float(scale), 0.0 if after is None else float(after.eps),
             0.0 if before is None else float(before.eps))
 

@@ -75,19 +75,21 @@ def _columns(x, name):
 
 
 def _check_packed(p, name, block=None):
-    """A Packed of the shapes that its columns and block say."""
+    """A Packed of the shapes that its columns and block say; gives the shape of its values."""
     if not isinstance(p, Packed):
         raise TypeError(f"{name} must be a Packed")
-    _block(p.block)
-    if block is not None and p.block != block:
-        raise ValueError(f"{name} must have a scale for {block or 'each row'}, got block = {p.block}")
-    _dev(p.values, f"{name}.values", torch.int8)
-    if p.values.dim() < 1 or p.columns < 1 or p.values.shape[-1] != _pitch(p.columns):
-        raise ValueError(f"{name}.values must be [..., {_pitch(p.columns)}] for {p.columns} columns, got "
-                         f"{list(p.values.shape)}")
-    if p.values.data_ptr() % 16:
+    values, scales, columns, own = p
+    _block(own)
+    if block is not None and own != block:
+        raise ValueError(f"{name} must have a scale for {block or 'each row'}, got block = {own}")
+    _dev(values, f"{name}.values", torch.int8)
+    shape = values.shape
+    if len(shape) < 1 or columns < 1 or shape[-1] != _pitch(columns):
+        raise ValueError(f"{name}.values must be [..., {_pitch(columns)}] for {columns} columns, got {list(shape)}")
+    if values.data_ptr() % 16:
         raise ValueError(f"{name}.values must be aligned to 16 bytes")
-    _match(p.scales, f"{name}.scales", p.values, _scales_shape(p.values.shape[:-1], p.columns, p.block), torch.float32)
+    _match(scales, f"{name}.scales", values, _scales_shape(shape[:-1], columns, own), torch.float32)
+    return shape
 
 
 def _run_pack(x, block):
@@ -150,51 +152,58 @@ def sinkhorn_expert_product_packed(x, weight, offsets=None, tokens=None, dtype=N
     Without offsets the weight is a Packed of [N, K] (or [1, N, K]) and every row is multiplied by it.  The sums are
     exact; dtype is the result's (float32, bfloat16 or float16; default: x's, bfloat16 for a Packed).  For serving: it
     has no gradient, and asking for one raises.  stream=: as in sinkhorn_forward."""
-    _check_packed(weight, "weight", 0)
-    shape = weight.values.shape
+    shape = _check_packed(weight, "weight", 0)
     if len(shape) == 2 and offsets is None:
         shape = (1, *shape)
     if len(shape) != 3 or (offsets is None and shape[0] != 1):
         raise ValueError(f"weight must be packed from [E, N, K] (without offsets from [N, K]), got values "
                          f"{list(weight.values.shape)}")
-    E, N, _ = shape
+    E, N, K = shape[0], shape[1], weight.columns
     if isinstance(x, Packed):
-        _check_packed(x, "x", 0)
-        rows, columns, given = x.values, x.columns, torch.bfloat16
+        rows, given, default = x.values, x.scales, torch.bfloat16
+        lead = _check_packed(x, "x", 0)[:-1]
+        columns = x.columns
     else:
-        x = x.contiguous()
-        _typed(x, "x")
-        rows, columns, given = x, x.shape[-1] if x.dim() else 0, x.dtype
-    if rows.dim() != 2 or columns != weight.columns:
-        raise ValueError(f"x must have rows of {weight.columns} columns, got {list(rows.shape[:-1]) + [columns]}")
+        rows = given = x = x.contiguous()
+        default = _typed(x, "x").dtype
+        *lead, columns = x.shape if x.dim() else (0,)
+    if len(lead) != 1 or columns != K:
+        raise ValueError(f"x must have rows of {K} columns, got {[*lead, columns]}")
     _match(weight.values, "weight", rows)
-    dtype = given if dtype is None else dtype
+    dtype = default if dtype is None else dtype
     if dtype not in _DTYPE:
         raise TypeError(f"dtype must be one of {[str(d) for d in _DTYPE]}, got {dtype}")
     if offsets is not None:
         _match(offsets, "offsets", rows, (E + 1,), torch.int32)
+    T = lead[0]
     if tokens is None:
-        T, k = _rows_in_order(rows.shape[0])
+        T, k = _rows_in_order(T)
     else:
         if offsets is None:
             raise ValueError("tokens go with offsets")
         _match(tokens, "tokens", rows, None, torch.int32)
-        T = rows.shape[0]
         k = _rows_of(tokens.numel(), T, "tokens")
-    sizes = T, k, E, weight.columns, N, _DTYPE[dtype]
-
-    def run(t, s):
-        packed = _run_pack(t, 0) if isinstance(x, torch.Tensor) else x
-        y = torch.empty((sizes[0] * sizes[1], N), device=rows.device, dtype=dtype)
-        _call(load_library().sinkhorn_experts_forward_packed, rows.device, _experts(*sizes)[0],
-              packed.values.data_ptr(), packed.scales.data_ptr(), weight.values.data_ptr(), s.data_ptr(),
-              _ptr(offsets), _ptr(tokens), y.data_ptr())
-        return y
-
-    given = rows if isinstance(x, torch.Tensor) else x.scales
+    call = x, weight, offsets, tokens, lead[0], (T, k, E, K, N, _DTYPE[dtype]), dtype
     if _recorded(given, weight.scales):
-        return _Constant.apply(run, "sinkhorn_expert_product_packed", given, weight.scales)
-    return run(given, weight.scales)
+        return _Constant.apply(functools.partial(_run_packed_product, *call), "sinkhorn_expert_product_packed", given,
+                               weight.scales)
+    return _run_packed_product(*call)
+
+
+def _run_packed_product(x, weight, offsets, tokens, rows, sizes, dtype, *_):
+    dev, lib = weight.values.device, load_library()
+    if isinstance(x, Packed):
+        values, scales = x.values.data_ptr(), x.scales.data_ptr()
+    else:  # the scales behind the values
+        wide = _pitch(x.shape[1])
+        space = torch.empty((rows * (wide + 4),), device=dev, dtype=torch.int8)
+        values = space.data_ptr()
+        scales = values + rows * wide
+        _call(lib.sinkhorn_pack, dev, _packing(rows, x.shape[1], 0, _DTYPE[x.dtype]), x.data_ptr(), values, scales)
+    y = torch.empty((sizes[0] * sizes[1], sizes[4]), device=dev, dtype=dtype)
+    _call(lib.sinkhorn_experts_forward_packed, dev, _experts(*sizes)[0], values, scales, weight.values.data_ptr(),
+          weight.scales.data_ptr(), _ptr(offsets), _ptr(tokens), y.data_ptr())
+    return y
 
 
 # ---- activations, and products that keep their rows in 8 bits ----
