@@ -14,6 +14,7 @@ from ._binding import (  # noqa: F401
     SinkhornError,
     library_path,
     load_library,
+    load_torch_library,
     sinkhorn_backward,
     sinkhorn_backward_points,
     sinkhorn_backward_sharp,
@@ -69,6 +70,7 @@ __all__ = [
     "SinkhornPointsLoss",
     "library_path",
     "load_library",
+    "load_torch_library",
     "sinkhorn_backward",
     "sinkhorn_backward_points",
     "sinkhorn_backward_sharp",

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib
 import os
 
 import torch
@@ -183,6 +184,21 @@ def load_library():
         getattr(lib, "sinkhorn_" + name).restype = ctypes.c_int
     _lib = lib
     return lib
+
+
+_torch = None
+
+
+def load_torch_library():
+    """Load _sinkhorn_torch.so, the library's calls on torch tensors; raises if it has not been built."""
+    global _torch
+    if _torch is None:
+        path = os.path.join(_HERE, "_sinkhorn_torch.so")
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is missing: build it with `python paper_1907_01729_amd/build.py` "
+                              "(or __graft_entry__.build()); there is no CPU fallback")
+        _torch = importlib.import_module("._sinkhorn_torch", __package__)
+    return _torch
 
 
 def _int32(*sizes, status=-2):

@@ -1,7 +1,9 @@
-"""Build the gfx950 HIP library ``libsinkhorn_hip.so`` in-tree with hipcc.
+"""Build the gfx950 HIP library ``libsinkhorn_hip.so`` in-tree with hipcc, and
+``_sinkhorn_torch.so``, the calls on torch tensors over it, with the host
+compiler against torch's headers.
 
 Each translation unit is compiled to an object in parallel (``_build/``), then
-the objects are linked into the shared library.  Every call compiles.
+the objects are linked into the shared libraries.  Every call compiles.
 """
 from __future__ import annotations
 
@@ -10,11 +12,13 @@ import os
 import shlex
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsinkhorn_hip.so")
+TORCH_LIB = os.path.join(HERE, "_sinkhorn_torch.so")
 OBJ_DIR = os.path.join(os.path.dirname(HERE), "_build")
 
 # Packed fp32 VALU forms are switched off for all device code (they are not
@@ -47,14 +51,16 @@ def _run(cmd, verbose):
         print(r.stderr, flush=True)
 
 
-def _compile_and_link(flags, obj_dir, lib, link_extra=(), verbose=False, jobs=None) -> str:
+def _compile_and_link(flags, obj_dir, lib, link_extra=(), verbose=False, jobs=None, beside=()) -> str:
+    """beside: commands that run next to the compilations."""
     os.makedirs(obj_dir, exist_ok=True)
     cc = hipcc()
     srcs = sources()
     objs = [os.path.join(obj_dir, os.path.basename(s)[:-4] + ".o") for s in srcs]
-    jobs = jobs or min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
+    jobs = jobs or min(len(srcs) + len(beside), max(1, min(16, os.cpu_count() or 1)))
     with ThreadPoolExecutor(max_workers=jobs) as ex:
-        futs = [ex.submit(_run, [cc, *flags, "-c", "-o", o, s], verbose) for s, o in zip(srcs, objs)]
+        futs = [ex.submit(_run, cmd, verbose) for cmd in beside]
+        futs += [ex.submit(_run, [cc, *flags, "-c", "-o", o, s], verbose) for s, o in zip(srcs, objs)]
         for f in futs:
             f.result()
     tmp = lib + ".tmp"
@@ -63,8 +69,30 @@ def _compile_and_link(flags, obj_dir, lib, link_extra=(), verbose=False, jobs=No
     return lib
 
 
+def _torch_commands():
+    """(compile, link) of the torch calls.  They are host code, which names HIP's stream type alone."""
+    import torch
+
+    root, cxx = os.path.dirname(torch.__file__), os.environ.get("CXX") or "g++"
+    obj = os.path.join(OBJ_DIR, "sk_torch.o")
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(rocm, "include")]
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    compile_ = [cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                f"-D_GLIBCXX_USE_CXX11_ABI={abi}", *(f"-I{d}" for d in include), "-c", "-o", obj,
+                os.path.join(CSRC, "sk_torch.cpp")]
+    link = [cxx, "-shared", "-o", TORCH_LIB + ".tmp", obj, "-L" + HERE, "-l:" + os.path.basename(LIB),
+            "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    return compile_, link
+
+
 def build(verbose: bool = False, jobs: int | None = None) -> str:
-    return _compile_and_link(HIP_FLAGS, OBJ_DIR, LIB, verbose=verbose, jobs=jobs)
+    compile_, link = _torch_commands()
+    lib = _compile_and_link(HIP_FLAGS, OBJ_DIR, LIB, verbose=verbose, jobs=jobs, beside=[compile_])
+    _run(link, verbose)
+    os.replace(TORCH_LIB + ".tmp", TORCH_LIB)
+    return lib
 
 
 # Host-side sanitizers for the CPU checks of the C ABI: AddressSanitizer and

@@ -7,7 +7,7 @@ import torch
 
 import paper_1907_01729_amd as sk
 from paper_1907_01729_amd import _binding as b
-from paper_1907_01729_amd import norm, packed
+from paper_1907_01729_amd import norm
 
 P = ctypes.c_void_p(0x1000)  # never dereferenced on the paths tested
 ODD = ctypes.c_void_p(0x1008)
@@ -133,11 +133,6 @@ def test_sizes_are_not_cut_off():
         for i in range(2):
             with pytest.raises(sk.SinkhornError):
                 norm._norms(*[n if i == j else 4 for j in range(2)], 1, 1, 0, 0, 0, 1, 1.0, 0.0, 0.0)
-        with pytest.raises(sk.SinkhornError):
-            packed._packing(4, n, 0, 1)
-    for n in (-1, 1 << 63, 1 << 64):
-        with pytest.raises(sk.SinkhornError):
-            packed._packing(n, 4, 0, 1)
 
 
 def test_wrappers_refuse_cpu_tensors():
