@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <mutex>
 #include <optional>
 #include <string>
 #include <tuple>
@@ -117,6 +118,7 @@ struct Node : torch::autograd::Node {
     bool wants(size_t i) const { return task_should_compute_output(i); }
 
     variable_list apply(variable_list &&grads) override {
+        const std::lock_guard<std::mutex> lock(mutex_);  // two backward passes through one graph
         const bool again = at::GradMode::is_enabled();
         for (const Tensor &g : grads) no_tangent(what, {g});
         variable_list out;
@@ -197,6 +199,7 @@ struct NormNode : Node {
         return {gx, gw, gb};
     }
     void release_variables() override {
+        const std::lock_guard<std::mutex> lock(mutex_);
         x.reset_data(), w.reset_data(), b.reset_data();
         stats.reset();
     }
@@ -271,6 +274,7 @@ struct ResidualNode : Node {
         return {same ? gr : gh, gr, gg, gaw, gab, gbw, gbb};
     }
     void release_variables() override {
+        const std::lock_guard<std::mutex> lock(mutex_);
         for (SavedVariable *v : {&h, &out, &gate, &aw, &ab, &bw, &bb}) v->reset_data();
         stats.reset();
     }
@@ -584,7 +588,10 @@ struct ActivationNode : Node {
         const On on(kept.values);
         return {activate_backward(kept, kind, gated, type, grads[0], false, on).second};
     }
-    void release_variables() override { kept.values.reset(), kept.scales.reset(); }
+    void release_variables() override {
+        const std::lock_guard<std::mutex> lock(mutex_);
+        kept.values.reset(), kept.scales.reset();
+    }
 };
 
 Tensor activation(const Tensor &x_, int64_t kind, bool gated) {
@@ -647,6 +654,7 @@ struct KeptNode : Node {
         return {gx, gw};
     }
     void release_variables() override {
+        const std::lock_guard<std::mutex> lock(mutex_);
         for (SavedVariable *v : {&weight, &offsets, &tokens, &slots}) v->reset_data();
         kept.values.reset(), kept.scales.reset();
     }

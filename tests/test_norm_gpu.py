@@ -380,3 +380,23 @@ def test_a_plain_sum_has_one_gradient_for_both():
         torch.autograd.backward((o, n), (g, g))
     want = (2 * both[0].float()).to(BF16)
     assert torch.equal(x.grad, want) and torch.equal(y.grad, want)
+
+
+def test_more_than_2_to_the_32_bytes():
+    """Rows whose bytes 32 bits do not count: those at the end are their own, forward and backward."""
+    T, N = 540000, 4096
+    h, w = torch.zeros(T, N, device="cuda", dtype=BF16), make(N, seed=1, plus=1.0, dtype=BF16)
+    h[:4], h[-4:] = rows(4, N, 3, BF16), rows(4, N, 5, BF16)
+    few = torch.cat((h[:4], h[-4:])).requires_grad_()
+    norm = sk.Norm(w, None, 1e-3)
+    small = sk.sinkhorn_residual_norm(few, few.detach(), None, 0.5, norm, norm)
+    g = torch.zeros_like(h)
+    g[:4], g[-4:] = rows(4, N, 7, BF16), rows(4, N, 9, BF16)
+    want, = torch.autograd.grad(small, few, [torch.cat((g[:4], g[-4:]))] * 2)
+    h.requires_grad_()
+    large = sk.sinkhorn_residual_norm(h, h.detach(), None, 0.5, norm, norm)
+    for a, b in zip(large, small):
+        assert torch.equal(torch.cat((a[:4], a[-4:])), b)
+        assert not a[4:-4].any()
+    got, = torch.autograd.grad(large, h, [g] * 2)
+    assert torch.equal(torch.cat((got[:4], got[-4:])), want) and not got[4:-4].any()
