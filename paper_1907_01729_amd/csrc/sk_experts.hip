@@ -54,11 +54,15 @@ __device__ __forceinline__ Sum4<T> mfma16(const Frag8<T> &a, const Frag8<T> &b, 
 // Elements past the end of the contraction come from a page of zeros; rows and columns past the tile's end repeat the
 // last one and are not stored.
 //
-// 65536 rows of 64 experts of 2048 x 2048, bf16: forward 509 us (1080 TFLOP/s), the input gradient's rows in 32 bits 561
-// (981), weight gradient 647 (849); a library product of 65536 x 2048 x 2048 reaches 1410 TFLOP/s here.  Of a step's
-// 1.55 us the products alone take 0.95 and the copies alone 1.28.  The LDS reads are not what bounds a step: 16-byte reads
+// 65536 rows of 64 experts of 2048 x 2048, bf16, equal shares: forward 487 us (1130 TFLOP/s), the input gradient's rows in
+// 32 bits 475 (1160), weight gradient 514 (1070); a library product of 65536 x 2048 x 2048 reaches 1410 TFLOP/s here.  Of
+// a step's 1.55 us the products alone take 0.95 and the copies alone 1.28.  The LDS reads are not what bounds a step: 16-byte reads
 // alone reach 248 bytes a cycle a CU, transposing ones 173, which for the weight gradient's 192 KB is a quarter of a step.
 // Rows that are no whole 16 bytes take 2 times as long forward and 3 to 4 times in the gradients.
+//
+// Rows in 8 bits: the same bytes hold twice the products.  65536 rows of 64 experts of 2048 x 2048 272 us with equal shares
+// (2020 TOP/s), of 4096 x 2048 (K = 4096) 490 (2240); a library product of 8192^3 in 8 bits reaches 2090 here.  Of a tile's
+// 31 us its 16 steps take 27.
 
 constexpr int kDeep = 64;
 
@@ -491,10 +495,12 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
             const Words4 v = *reinterpret_cast<const Words4 *>(lds + r * kPitch + c % kChunks * 16);
             char *out = sizeof(O) == 4 ? reinterpret_cast<char *>(A.out32) : static_cast<char *>(A.out);
             out += ((row0 + row) * cols + col) * (int)sizeof(O);
-            if (whole_out) {
-                // Not kept in L2, where a round's results would push out the operands: 65536 rows of 64 experts of
-                // 2048 x 1024 in 8 bits in 160 us, kept 188; in 16 bits, 32768 rows of 16 of 2048 x 1024 forward and
-                // backward, 3 % less.
+            if (whole_out && MODE == kWeight && A.out32) {
+                *reinterpret_cast<Words4 *>(out) = v;  // parts, which are read again at once (32768 x 128 x 128: 19 / 26 us)
+            } else if (whole_out) {
+                // Not kept in L2, where a round's results would push out the operands.  Kept / not, in us: 65536 rows of
+                // 64 experts of 2048 x 1024 in 8 bits 188 / 160; 32768 of 16 of 2048 x 1024 in 16 bits forward 153 / 142,
+                // input gradient 166 / 141; weight gradient of 65536 of 64 of 2048 x 2048 546 / 514.
                 __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), reinterpret_cast<i32x4 *>(out));
             } else if (cols - col >= kEach) {
                 __builtin_memcpy(out, &v, 16);
@@ -526,7 +532,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 // many wavefronts have to ask for them at once.  A work-group takes kFewCols columns, and its four wavefronts a quarter
 // of the contraction each, straight from memory to registers; their sums meet in LDS.  A lane's 32 bytes of a row's 128
 // are two fragments: the products' order along the contraction is free as long as both factors have the same.  16 rows
-// of 14 of 64 experts of 1024 x 2048: 59 MB in 13 us (4.5 TB/s); in tiles of 64 18 us.
+// of 14 of 64 experts of 1024 x 2048: 59 MB in 13 us (4.5 TB/s); in tiles of 64 18 us.  In 8 bits: 30 MB in 9 us.
 
 constexpr int kFewRows = 16, kFewCols = 32, kFewChunk = 64, kFewAtOnce = 4;
 
@@ -687,9 +693,10 @@ struct Cut {
 // Rows' products.  The expected number of tiles (half a tile of each expert is empty) decides.  256: one work-group a
 // CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each other's first
 // copies and last writes.  64: too few tiles of 128 to go round.  Measured, 256 / 128 / 64, in us: 65536 rows of 64
-// experts of 2048 x 2048 (9.0 rounds) 527 / 609 / 914; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 147 / 143 / 205; 8000
-// rows of 2 of 2048 x 1024 (1.0) 34 / 39 / 62; 2331 rows of 12 of 520 x 1000 25 / 12.5 / 11.6; 300 rows of 2 of
-// 2048 x 2048 40 / 17 / 12.
+// experts of 2048 x 2048 (9.0 rounds) 535 / 611 / 916; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 161 / 159 / 223; 8000
+// rows of 2 of 2048 x 1024 (1.0) 32 / 39 / 53; 2331 rows of 12 of 520 x 1000 24 / 15 / 12; 300 rows of 2 of
+// 2048 x 2048 39 / 21 / 16.  Equal shares of whole tiles come out even better in 256 (8192 rows of 8: 118 / 147), but how
+// the shares are is known on the device alone.
 Cut cut_rows(const ExpertArgs &a, int cols) {
     const int64_t rows = (int64_t)a.T * a.k;
     auto tiles = [&](int64_t tile) { return (rows / tile + (a.E + 1) / 2) * parts_of(cols, tile); };
@@ -700,9 +707,9 @@ Cut cut_rows(const ExpertArgs &a, int cols) {
 
 // Weight gradients.  256 where there are two rounds of it and its edges waste no more than 128's would; else 128, or 64
 // where that makes too few work-groups.  Few tiles over many rows are cut along the rows, into parts of eight steps or
-// more, until there are two work-groups a CU.  Measured, in us: 256 / 128: 8192 rows of 8 of 4096 x 2048 197 / 231,
-// 24000 rows of 32 of 2048 x 1024 147 / 174; 128 / 64: 9620 rows of 14 of 96 x 80 16.4 / 10.9; whole / in parts: 65536
-// rows of 16 experts of 512 x 512 111 / 73, 32768 rows of 2 of 128 x 128 131 / 19, of 128 x 127 809 / 45.
+// more, until there are two work-groups a CU.  Measured, in us: 256 / 128: 8192 rows of 8 of 4096 x 2048 121 / 140,
+// 24000 rows of 32 of 2048 x 1024 98 / 106; 128 / 64: 9620 rows of 14 of 96 x 80 8.7 / 6.4; whole / in parts: 65536
+// rows of 16 experts of 512 x 512 46 / 46, 32768 rows of 2 of 128 x 128 81 / 19, of 128 x 127 786 / 43.
 Cut cut_weight(const ExpertArgs &a) {
     auto tiles = [&](int64_t tile) { return a.E * parts_of(a.N, tile) * parts_of(a.K, tile); };
     if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1};
@@ -798,9 +805,9 @@ size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
     // The weights are read once for each 16 rows of an expert.  Few / tiles, in us: 256 rows, 64 experts of 2048 x 2048
-    // 95 / 115; 512 rows, 64 of 1024 x 1024 34 / 28.  Up to 64 rows of few experts, too, where tiles are too few: 64 rows
-    // of one of 2048 x 2048 9.0 / 11.3, of 4096 x 4096 25 / 32, of 512 x 512 4.8 / 5.5; of four of 2048 x 2048 9.6 / 17.
-    // Only large matrices have tiles enough then: 32 rows of 8192 x 8192 45 / 57, but 64 rows 87 / 61.
+    // 99 / 122; 512 rows, 64 of 1024 x 1024 32 / 26.  Up to 64 rows of few experts, too, where tiles are too few: 64 rows
+    // of one of 2048 x 2048 8.5 / 17, of 4096 x 4096 24 / 31, of 512 x 512 4.5 / 5.2; of four of 2048 x 2048 14 / 17.
+    // Only large matrices have tiles enough then: 32 rows of 8192 x 8192 57 / 90, but 64 rows 98 / 93.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, a.N), st);
@@ -810,6 +817,9 @@ hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
     ExpertArgs a = p;
     a.whole_out = aligned16(a.out) && (int64_t)a.N * (a.dtype == SK_F32 ? 4 : 2) % 16 == 0;
     a.out32 = a.dtype == SK_F32 ? static_cast<float *>(a.out) : nullptr;
+    // The rules of 16-bit rows.  Few / tiles here, in us: 64 rows of one of 2048 x 2048 6.1 / 7.2, of 4096 x 4096
+    // 14.5 / 17.3, of 8192 x 8192 52 / 49; 128 rows of one of 4096 x 4096 25 / 17; 256 rows of 64 of 2048 x 2048
+    // 51.5 / 51.5, 384 rows 56 / 52.
     const int64_t rows = (int64_t)a.T * a.k;
     if (rows <= 64 || rows <= 4 * a.E) {
         const dim3 grid((unsigned)(parts_of(most_row_tiles(a, kFewRows) * parts_of(a.N, kFewCols), 8) * 8));

