@@ -506,7 +506,7 @@ typedef struct {
 
 /*
  * Norm of x [T, N] by p->before (not SK_NORM_NONE) with eps_before; the gate,
- * `after` and the scale are not used.  stats [T, 4] (may be NULL without a
+ * `after` and the scale are not used (0, for the workspace's size below).  stats [T, 4] (may be NULL without a
  * backward pass) keeps the rows' means and r.
  */
 SK_API sk_status sinkhorn_norm_forward(const sk_norms *p, const void *x, const void *w, const void *b, void *y,

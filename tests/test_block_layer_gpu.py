@@ -178,3 +178,20 @@ def test_calls_under_inference_mode_and_many_threads():
     torch.cuda.synchronize()
     for v in got:
         assert torch.equal(v, want)
+
+
+def test_on_another_stream():
+    """Forward and backward on a side stream, what they leave behind used there again at once."""
+    b, x = block(), rows(300).requires_grad_()
+    g = torch.randn_like(x)
+    leaves = [x, *b.parameters()]
+    want = torch.autograd.grad(b(x, 0)[0], leaves, g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(5):
+            got = torch.autograd.grad(b(x, 0)[0], leaves, g)
+            torch.full((1 << 20,), float("nan"), device="cuda")  # takes what was freed
+    torch.cuda.synchronize()
+    for u, v in zip(got, want):
+        assert torch.equal(u, v)

@@ -400,3 +400,16 @@ def test_more_than_2_to_the_32_bytes():
         assert not a[4:-4].any()
     got, = torch.autograd.grad(large, h, [g] * 2)
     assert torch.equal(torch.cat((got[:4], got[-4:])), want) and not got[4:-4].any()
+
+
+@pytest.mark.parametrize("T,N", [(2, 16392), (1, 33000), (3, 40001)])
+@pytest.mark.parametrize("dtype,kinds", [(BF16, ("rms", "rms")), (F32, ("centred", "centred")), (F16, ("", "rms"))])
+def test_block_ends_of_very_wide_rows(T, N, dtype, kinds):
+    """More columns than the lanes hold: the sum is read again from where it has been written."""
+    check_block(T, N, dtype, dtype, "none", F32, *kinds)
+
+
+def test_many_wide_rows():
+    """Several rows to a work-group whose sums lie in memory."""
+    check_block(600, 8200, BF16, BF16, "channel", BF16, "centred", "rms")
+    check_norm(530, 9001, F32, F32, True)
