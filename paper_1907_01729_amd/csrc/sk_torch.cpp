@@ -3,6 +3,7 @@
 // norm with its gradients takes the host 45 us a step, with a node written in Python 105.
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/VariableTypeUtils.h>
 #include <torch/csrc/autograd/function.h>
@@ -117,8 +118,22 @@ struct Node : torch::autograd::Node {
     virtual variable_list gradients(const variable_list &grads) = 0;
     bool wants(size_t i) const { return task_should_compute_output(i); }
 
+    // The engine has the stream of whoever takes a gradient wait for the stream of this node.  While this one is captured
+    // and that one is the default stream, as of a leaf that an eager graph still holds, the wait cannot be recorded, and
+    // the error ends the process.
+    void check_capture() const {
+        if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+        for (size_t i = 0; i < num_outputs(); ++i) {
+            if (!next_edge(i).is_valid() || !wants(i)) continue;
+            const auto taker = next_edge(i).function->stream();
+            TORCH_CHECK(!taker || taker->id() != 0, what, ": a backward pass cannot be captured while a graph made on the "
+                        "default stream holds one of its leaves; delete that graph's results first");
+        }
+    }
+
     variable_list apply(variable_list &&grads) override {
         const std::lock_guard<std::mutex> lock(mutex_);  // two backward passes through one graph
+        check_capture();
         const bool again = at::GradMode::is_enabled();
         for (const Tensor &g : grads) no_tangent(what, {g});
         variable_list out;
@@ -179,29 +194,27 @@ void rows(const Tensor &t, const char *name) {
 }
 
 struct NormNode : Node {
-    SavedVariable x, w, b;
-    Tensor stats;
+    SavedVariable x, w, b, stats;
     sk_norms p;
     NormNode() : Node("sinkhorn_norm") {}
 
     variable_list gradients(const variable_list &grads) override {
         if (!grads[0].defined()) return variable_list(3);
-        const Tensor xv = x.unpack(), wv = w.unpack(), bv = b.unpack();
+        const Tensor xv = x.unpack(), wv = w.unpack(), bv = b.unpack(), sv = stats.unpack();
         const On on(xv);
         const Tensor gx = wants(0) ? at::empty_like(xv) : Tensor(),
                      gw = wv.defined() && wants(1) ? at::empty_like(wv) : Tensor(),
                      gb = bv.defined() && wants(2) ? at::empty_like(bv) : Tensor();
         const size_t need = gw.defined() || gb.defined() ? sinkhorn_norm_workspace_bytes(&p) : 0;
         const Tensor ws = empty_bytes(need, xv);
-        check(sinkhorn_norm_backward(&p, data(xv), data(wv), data_of<float>(stats), data(grads[0]), data(gx), data(gw),
+        check(sinkhorn_norm_backward(&p, data(xv), data(wv), data_of<float>(sv), data(grads[0]), data(gx), data(gw),
                                      data(gb), data(ws), need, on.stream),
               "sinkhorn_norm_backward");
         return {gx, gw, gb};
     }
     void release_variables() override {
         const std::lock_guard<std::mutex> lock(mutex_);
-        x.reset_data(), w.reset_data(), b.reset_data();
-        stats.reset();
+        for (SavedVariable *v : {&x, &w, &b, &stats}) v->reset_data();
     }
 };
 
@@ -231,15 +244,14 @@ Tensor norm(const Tensor &x_, const NormOf &norm_) {
     if (rec) {
         auto node = new_node<NormNode>();
         node->x = keep(x), node->w = keep(n.w), node->b = keep(n.b);
-        node->stats = stats, node->p = p;
+        node->stats = keep(stats), node->p = p;
         attach(node, {y}, torch::autograd::collect_next_edges(x, n.w, n.b));
     }
     return y;
 }
 
 struct ResidualNode : Node {
-    SavedVariable h, out, gate, aw, ab, bw, bb;
-    Tensor stats;
+    SavedVariable h, out, gate, aw, ab, bw, bb, stats;
     sk_norms p;
     bool has_out = false;
     at::TensorOptions options;
@@ -249,11 +261,9 @@ struct ResidualNode : Node {
         const Tensor g_out = grads[0], g_next = grads.size() > 1 ? grads[1] : Tensor();
         if (!g_out.defined() && !g_next.defined()) return variable_list(7);
         const Tensor hv = h.unpack(), gv = gate.unpack(), awv = aw.unpack(), abv = ab.unpack(), bwv = bw.unpack(),
-                     bbv = bb.unpack();
+                     bbv = bb.unpack(), sv = stats.unpack();
         const Tensor ov = has_out ? out.unpack(shared_from_this()) : Tensor();
-        TORCH_CHECK(stats.defined(), "sinkhorn_residual_norm: what was kept for the backward pass is released; "
-                                     "retain_graph=True keeps it for another one");
-        const On on(stats);
+        const On on(sv);
         auto made = [&](size_t i, const Tensor &as) {
             return as.defined() && wants(i) ? at::empty_like(as) : Tensor();
         };
@@ -265,9 +275,9 @@ struct ResidualNode : Node {
         const bool sums = gaw.defined() || gab.defined() || gbw.defined() || gbb.defined() ||
                           (gg.defined() && p.gate == SK_GATE_COLUMNS);
         const size_t need = sums ? sinkhorn_norm_workspace_bytes(&p) : 0;
-        const Tensor ws = empty_bytes(need, stats);
+        const Tensor ws = empty_bytes(need, sv);
         check(sinkhorn_residual_norm_backward(&p, data(hv), data(ov), data(gv), data(awv), data(abv), data(bwv),
-                                              data_of<float>(stats), data(g_out), data(g_next), data(gh), data(gr),
+                                              data_of<float>(sv), data(g_out), data(g_next), data(gh), data(gr),
                                               data(gg), data(gaw), data(gab), data(gbw), data(gbb), data(ws), need,
                                               on.stream),
               "sinkhorn_residual_norm_backward");
@@ -275,8 +285,7 @@ struct ResidualNode : Node {
     }
     void release_variables() override {
         const std::lock_guard<std::mutex> lock(mutex_);
-        for (SavedVariable *v : {&h, &out, &gate, &aw, &ab, &bw, &bb}) v->reset_data();
-        stats.reset();
+        for (SavedVariable *v : {&h, &out, &gate, &aw, &ab, &bw, &bb, &stats}) v->reset_data();
     }
 };
 
@@ -337,7 +346,7 @@ variable_list residual_norm(const Tensor &h_, const Tensor &residual_, const May
         if (after_ || (gate.defined() && gate.requires_grad())) node->h = keep(h);
         node->gate = keep(gate), node->aw = keep(after.w), node->ab = keep(after.b);
         node->bw = keep(before.w), node->bb = keep(before.b);
-        node->stats = stats, node->p = p, node->options = h.options();
+        node->stats = keep(stats), node->p = p, node->options = h.options();
         attach(node, results,
                torch::autograd::collect_next_edges(h, residual, gate, after.w, after.b, before.w, before.b));
         if (before_) node->out = SavedVariable(out, true), node->has_out = true;
@@ -575,22 +584,31 @@ std::pair<Tensor, Tensor> activate_backward(const Packed &kept, int64_t kind, bo
     return {y, gx};
 }
 
+// Rows that a node keeps: as saved tensors, so that hooks on those (checkpoints, copies to the host) have them too.
+struct KeptRows {
+    SavedVariable values, scales;
+    int64_t columns = 0;
+    KeptRows() = default;
+    explicit KeptRows(const Packed &p) : values(keep(p.values)), scales(keep(p.scales)), columns(p.columns) {}
+    Packed unpack() const { return {values.unpack(), scales.unpack(), columns, kKeptBlock}; }
+    void release() { values.reset_data(), scales.reset_data(); }
+};
+
 struct ActivationNode : Node {
-    Packed kept;
+    KeptRows rows;
     int64_t kind;
     bool gated;
     at::ScalarType type;
     ActivationNode() : Node("sinkhorn_activation") {}
     variable_list gradients(const variable_list &grads) override {
         if (!grads[0].defined()) return variable_list(1);
-        TORCH_CHECK(kept.values.defined(), "sinkhorn_activation: the rows kept for the backward pass are released; "
-                                           "retain_graph=True keeps them for another one");
+        const Packed kept = rows.unpack();
         const On on(kept.values);
         return {activate_backward(kept, kind, gated, type, grads[0], false, on).second};
     }
     void release_variables() override {
         const std::lock_guard<std::mutex> lock(mutex_);
-        kept.values.reset(), kept.scales.reset();
+        rows.release();
     }
 };
 
@@ -609,7 +627,7 @@ Tensor activation(const Tensor &x_, int64_t kind, bool gated) {
     }
     if (rec) {
         auto node = new_node<ActivationNode>();
-        node->kept = kept, node->kind = kind, node->gated = gated, node->type = x.scalar_type();
+        node->rows = KeptRows(kept), node->kind = kind, node->gated = gated, node->type = x.scalar_type();
         attach(node, {y}, torch::autograd::collect_next_edges(x));
     }
     return y;
@@ -617,7 +635,7 @@ Tensor activation(const Tensor &x_, int64_t kind, bool gated) {
 
 struct KeptNode : Node {
     SavedVariable weight, offsets, tokens, slots;
-    Packed kept;
+    KeptRows rows;
     int64_t kind;
     bool gated;
     sk_experts p;
@@ -627,12 +645,12 @@ struct KeptNode : Node {
     variable_list gradients(const variable_list &grads) override {
         if (!grads[0].defined()) return variable_list(2);
         const Tensor w = weight.unpack(), off = offsets.unpack(), tok = tokens.unpack(), sl = slots.unpack();
+        const Packed kept = rows.unpack();
         const Tensor &gy = grads[0];
         const On on(w);
-        const int64_t rows = static_cast<int64_t>(p.T) * p.k;
         Tensor gx, a, gw;
         if (wants(0)) {
-            gx = empty({sl.defined() ? p.T : rows, p.K}, w, type);
+            gx = empty({sl.defined() ? p.T : static_cast<int64_t>(p.T) * p.k, p.K}, w, type);
             const size_t need = sl.defined() ? sinkhorn_experts_workspace_bytes(&p) : 0;
             const Tensor ws = empty_bytes(need, w);
             check(sinkhorn_experts_backward_input(&p, data(gy), data(w), data_of<int32_t>(off), data_of<int32_t>(sl),
@@ -656,7 +674,7 @@ struct KeptNode : Node {
     void release_variables() override {
         const std::lock_guard<std::mutex> lock(mutex_);
         for (SavedVariable *v : {&weight, &offsets, &tokens, &slots}) v->reset_data();
-        kept.values.reset(), kept.scales.reset();
+        rows.release();
     }
 };
 
@@ -709,7 +727,7 @@ Tensor product_kept(const Tensor &x_, const Tensor &weight_, const Tensor &offse
     if (rec) {
         auto node = new_node<KeptNode>();
         node->weight = keep(weight), node->offsets = keep(offsets), node->tokens = keep(tokens);
-        node->slots = keep(slots), node->kept = kept, node->kind = kind, node->gated = gated, node->p = p;
+        node->slots = keep(slots), node->rows = KeptRows(kept), node->kind = kind, node->gated = gated, node->p = p;
         node->type = x.scalar_type();
         attach(node, {y}, torch::autograd::collect_next_edges(x, weight));
     }

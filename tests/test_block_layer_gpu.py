@@ -195,3 +195,73 @@ def test_on_another_stream():
     torch.cuda.synchronize()
     for u, v in zip(got, want):
         assert torch.equal(u, v)
+
+
+def test_what_is_kept_goes_through_hooks_on_saved_tensors():
+    """Saved on the host and brought back: the same gradients, and nothing of the rows' size left on the GPU."""
+    b, x = block(), rows(4000).requires_grad_()
+    g = torch.randn_like(x)
+    leaves = [x, *b.parameters()]
+    want = torch.autograd.grad(b(x, 0)[0], leaves, g)
+    seen = []
+
+    def pack(t):
+        seen.append(t.dtype)
+        return t.to("cpu")
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.to("cuda")):
+        y = b(x, 0)[0]
+    got = torch.autograd.grad(y, leaves, g)
+    assert torch.int8 in seen
+    for u, v in zip(got, want):
+        assert torch.equal(u, v)
+    for call in (lambda: sk.sinkhorn_norm(x), lambda: sk.sinkhorn_residual_norm(x, x, before=sk.Norm())[1],
+                 lambda: sk.sinkhorn_activation(x, "silu")):
+        want, = torch.autograd.grad(call(), x, g)
+        call()
+        before = torch.cuda.memory_allocated()
+        with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.to("cuda")):
+            y = call()
+        assert torch.cuda.memory_allocated() - before <= 2 * y.numel() * y.element_size()  # y, and what it is the norm of
+        assert torch.equal(torch.autograd.grad(y, x, g)[0], want)
+
+
+def test_under_a_checkpoint():
+    from torch.utils.checkpoint import checkpoint
+    b, x = block(), rows(4000).requires_grad_()
+    g = torch.randn_like(x)
+    leaves = [x, *b.parameters()]
+    y = b(x, 0)[0]
+    want = torch.autograd.grad(y, leaves, g)
+    before = torch.cuda.memory_allocated()
+    again = checkpoint(lambda v: b(v, 0)[0], x, use_reentrant=False)
+    # The result alone is left, up to what the allocator rounds.
+    assert torch.cuda.memory_allocated() - before <= y.numel() * y.element_size() + 4096
+    assert torch.equal(again, y)
+    for u, v in zip(torch.autograd.grad(again, leaves, g), want):
+        assert torch.equal(u, v)
+
+
+def test_a_captured_backward_pass_beside_an_eager_graph_is_refused():
+    """The default stream cannot wait for a captured one; once the eager graph is gone the capture goes through."""
+    x = rows(40).requires_grad_()
+    w = torch.ones(1, 64, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    offsets = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    g = torch.randn_like(x)
+    for call in (lambda: sk.sinkhorn_norm(x), lambda: sk.sinkhorn_residual_norm(x, x), lambda: sk.sinkhorn_activation(x, "silu"),
+                 lambda: sk.sinkhorn_expert_product_kept(x, w, offsets)):
+        eager = call()
+        want, = torch.autograd.grad(eager, x, g, retain_graph=True)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="cannot be captured"):
+            with torch.cuda.graph(graph):
+                torch.autograd.grad(call(), x, g)
+        del eager, graph
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got, = torch.autograd.grad(call(), x, g)
+        for _ in range(3):
+            got.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
