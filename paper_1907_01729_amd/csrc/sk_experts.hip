@@ -39,8 +39,9 @@ __device__ __forceinline__ Sum4<T> mfma16(const Frag8<T> &a, const Frag8<T> &b, 
 //
 // A work-group computes BM x BN results; its wavefronts, WM x WN of them, a part of BM / WM x BN / WN each, held in
 // registers.  The contraction goes in steps of 64 (128 bytes of a row, a whole cache line).  Operands are copied to LDS
-// by the memory pipe itself, 16 bytes a lane, into one of two buffers, one step ahead of the products, with one barrier
-// a step.  The copies are issued one by one among the products, since the pipe takes few at a time and a wavefront
+// by the memory pipe itself, 16 bytes a lane, into the next of BUFFERS buffers, so many steps less one ahead of the
+// products, with one barrier a step.  Two buffers where several work-groups a CU cover each other's waits, more where one
+// or two have the CU to themselves (Cut, below).  The copies are issued one by one among the products, since the pipe takes few at a time and a wavefront
 // whose copy is not taken cannot issue its products; they are addressed by a scalar base and an offset of 32 bits a
 // lane, which the pipe takes a tenth faster than addresses of 64 bits.
 //
@@ -75,7 +76,7 @@ using LdsShort4 = __attribute__((address_space(3))) s16x4;
 
 // Copies 16 bytes a lane to LDS: from base + each lane's offset to `to` (one for the wavefront) + 16 lane.  WIDE: the
 // offset is a whole address.  Written out, since the compiler puts a wait for every copy under way before each
-// transposing read that follows it.  It has no result in registers, and the place is not read before all_copies.
+// transposing read that follows it.  It has no result in registers, and the place is not read before copies_landed.
 template <bool WIDE>
 using Offset = std::conditional_t<WIDE, const char *, uint32_t>;
 
@@ -93,10 +94,15 @@ __device__ __forceinline__ void copy16(const char *base, Offset<WIDE> from, char
                      : "v"(from), "s"(place), "s"(base)
                      : "m0", "memory");
 }
-// Every copy of the work-group has landed and every LDS read is done.
-__device__ __forceinline__ void all_copies() {
+// Every copy of the work-group has landed but the last `later` steps' ones, of EACH a wavefront (each wavefront waits for
+// its own; loads land in order), and every LDS read is done.  later <= MOST.
+template <int EACH, int MOST>
+__device__ __forceinline__ void copies_landed(int later) {
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (MOST == 0 || later == MOST)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(EACH * MOST) : "memory");
+    else if constexpr (MOST > 0)
+        copies_landed<EACH, MOST - 1>(later);
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -177,7 +183,7 @@ __device__ __forceinline__ Frag8<T> load_chunk(const T *p, int count) {
 // GATHERED: x's rows are looked up in tokens.  WIDE: x has 2^32 bytes or more.  STAGED: rows that are no whole chunks of
 // 16 bytes, or pointers that are not aligned to them: the chunks come through registers, loaded at the start of a step
 // and written to LDS at its end.
-template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE, bool STAGED>
+template <class T, int MODE, int BM, int BN, int WM, int WN, bool GATHERED, bool WIDE, bool STAGED, int BUFFERS = 2>
 __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void sk_experts_tile(ExpertArgs A) {
     constexpr int WAVES = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
     using OpA = Operand<T, MODE == kWeight, BM, WAVES, FM>;
@@ -186,7 +192,9 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     constexpr bool kWideA = WIDE && MODE == kForward, kWideB = WIDE && MODE == kWeight;
     constexpr int kOut = BM * (BN * 2 + 32);  // the results, below
     static_assert(BM / WM * (BN * 4 + 32) <= kOut);
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStep > kOut ? 2 * kStep : kOut];
+    constexpr int kLds = BUFFERS * kStep;
+    static_assert(BUFFERS == 2 || (!STAGED && MODE != kWeight));  // those have one step's chunks or rows at hand
+    __shared__ __attribute__((aligned(1024))) char lds[kLds > kOut ? kLds : kOut];
 
     __shared__ __attribute__((aligned(16))) float scales[kPairs<T> ? BM + BN : 1];  // of the tile's rows and columns
 
@@ -378,10 +386,11 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         // copies, if there is one: all in the first half, so that they land during the second (over all turns: 4 %
         // slower).  The compiler may not move anything across turns, or it would read each fragment right before its
         // use and wait for it.
-        auto step = [&](auto next, auto partial, int d0, const char *here, char *there) {
+        constexpr int kAhead = (BUFFERS - 1) * kDeep;
+        auto step = [&](auto next, auto partial, int later, int d0, const char *here, char *there) {
             constexpr int kTurns = kDeep / 32 * FM, kLead = 2, kEach = kCopies / (kTurns / 2);
             static_assert(kEach * (kTurns / 2) == kCopies && FM >= FN);
-            all_copies();
+            copies_landed<kCopies, BUFFERS - 2>(later);
             take_rows();
             look_up(d0 + 2 * kDeep);
             const char *la = here, *lb = here + OpA::kBytes;
@@ -399,7 +408,7 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
                 if constexpr (decltype(next)::value) {
                     if (i < kTurns / 2) {
 #pragma unroll
-                        for (int c = i * kEach; c < (i + 1) * kEach; ++c) copy(partial, c, d0 + kDeep, there);
+                        for (int c = i * kEach; c < (i + 1) * kEach; ++c) copy(partial, c, d0 + kAhead, there);
                     }
                 }
                 __builtin_amdgcn_s_setprio(1);  // before the other wavefront's reads and copies
@@ -416,28 +425,41 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         look_up(0);
         take_rows();
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c) copy(yes, c, 0, lds);
-        put(lds);
-        advance();
+        for (int b = 0; b < BUFFERS - 1; ++b) {
+            if (b && b * kDeep >= deep) break;
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c) copy(yes, c, b * kDeep, lds + b * kStep);
+            put(lds);
+            advance();
+        }
         look_up(kDeep);
         auto run = [&](auto one_step) {
-            int d0 = 0, odd = 0;
-            for (; d0 + 2 * kDeep <= deep; d0 += kDeep, odd ^= 1)
-                one_step(yes, no, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
-            if (d0 + kDeep < deep) {
-                one_step(yes, yes, d0, lds + odd * kStep, lds + (odd ^ 1) * kStep);
-                d0 += kDeep, odd ^= 1;
+            int d0 = 0, here = 0, there = (BUFFERS - 1) * kStep;
+            auto on = [&] {
+                d0 += kDeep;
+                there = here;
+                here = here + kStep == kLds ? 0 : here + kStep;
+            };
+            for (; d0 + kAhead + kDeep <= deep; on()) one_step(yes, no, BUFFERS - 2, d0, lds + here, lds + there);
+            if (d0 + kAhead < deep) {
+                one_step(yes, yes, BUFFERS - 2, d0, lds + here, lds + there);
+                on();
             }
-            one_step(no, no, d0, lds + odd * kStep, lds);
+            if constexpr (BUFFERS == 2) {
+                one_step(no, no, 0, d0, lds + here, lds);
+            } else {
+                for (; d0 < deep; on())
+                    one_step(no, no, min((deep - d0 - 1) / kDeep, BUFFERS - 2), d0, lds + here, lds);
+            }
         };
         if (idle)
-            run([&](auto next, auto partial, int d0, const char *, char *there) {
-                all_copies();
+            run([&](auto next, auto partial, int later, int d0, const char *, char *there) {
+                copies_landed<kCopies, BUFFERS - 2>(later);
                 take_rows();
                 look_up(d0 + 2 * kDeep);
                 if constexpr (decltype(next)::value) {
 #pragma unroll
-                    for (int c = 0; c < kCopies; ++c) copy(partial, c, d0 + kDeep, there);
+                    for (int c = 0; c < kCopies; ++c) copy(partial, c, d0 + kAhead, there);
                     put(there);
                 }
                 advance();
@@ -685,24 +707,38 @@ int64_t most_row_tiles(const ExpertArgs &a, int tile) {
     return rows / tile + (rows < a.E + 1 ? rows : a.E + 1);
 }
 
-// How a product is cut: tiles of `tile` squared, the weight gradient's rows in `parts`.
+// How a product is cut: tiles of `tile` squared with `buffers` steps of operands in LDS, the weight gradient's rows in
+// `parts`.
 struct Cut {
-    int tile, parts;
+    int tile, parts, buffers;
 };
 
-// Rows' products.  The expected number of tiles (half a tile of each expert is empty) decides.  256: one work-group a
-// CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each other's first
-// copies and last writes.  64: too few tiles of 128 to go round.  Measured, 256 / 128 / 64, in us: 65536 rows of 64
-// experts of 2048 x 2048 (9.0 rounds) 535 / 611 / 916; 8192 rows of 8 of 4096 x 2048 (2.3 rounds) 161 / 159 / 223; 8000
-// rows of 2 of 2048 x 1024 (1.0) 32 / 39 / 53; 2331 rows of 12 of 520 x 1000 24 / 15 / 12; 300 rows of 2 of
-// 2048 x 2048 39 / 21 / 16.  Equal shares of whole tiles come out even better in 256 (8192 rows of 8: 118 / 147), but how
-// the shares are is known on the device alone.
-Cut cut_rows(const ExpertArgs &a, int cols) {
+// Rows' products.  The expected number of tiles (half a tile of each of several experts is empty) decides.  256: one
+// work-group a CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each
+// other's first copies and last writes, or one with another step of copies under way.  64: too few tiles of 128 to go
+// round.  What is under way bounds those, so they have as many buffers as let all tiles run at once: four up to two a CU,
+// three up to three.
+// Measured, 256 / 128 / 64, in us: 65536 rows of 64 experts of 2048 x 2048 (9.0 rounds) 535 / 611 / 916; 8192 rows of 8 of
+// 4096 x 2048 (2.3 rounds) 161 / 159 / 223; 8000 rows of 2 of 2048 x 1024 (1.0) 32 / 39 / 53.  Equal shares of whole tiles
+// come out even better in 256 (8192 rows of 8: 118 / 147), but how the shares are is known on the device alone.
+// 128 with two buffers / with three / 64 with four: in 8 bits, rows of one of 8192 x 8192: 256 49 / 35 / 30, 512 53 / 39 / 57,
+// 1024 65 / 74 / 107; 1024 rows of one of 4096 x 4096 26 / 21 / 31, 512 of it 23 / 18 / 17; 2331 rows of 12 of 520 x 1008
+// 9.8 / 9.0 / 8.0, 5000 10.3 / 9.9 / 11.6; in 16 bits, 512 rows of one of 8192 x 8192 112 / 88 / 115; 600 rows of 4 of
+// 2048 x 2048 22 / 23 / 14.  64 with two / four: 8 bits, 256 rows of one of 4096 x 4096 17 / 9.6; 16 bits, 256 of one of
+// 2048 x 2048 16 / 8.8, 128 of one of 8192 x 8192 93 / 43; two / three / four, 8 bits, 4000 rows of 64 of 512 x 512 (2.9 a
+// CU) 6.9 / 7.0 / 8.4.  128 with three in the input gradient, two / three: 1024 rows of one of 4096 x 4096 45 / 50, 512 of
+// 8192 x 8192 105 / 96: two.
+Cut cut_rows(const ExpertArgs &a, bool input) {
+    const int cols = input ? a.K : a.N;
     const int64_t rows = (int64_t)a.T * a.k;
-    auto tiles = [&](int64_t tile) { return (rows / tile + (a.E + 1) / 2) * parts_of(cols, tile); };
+    auto tiles = [&](int64_t tile) {
+        return (a.E == 1 ? parts_of(rows, tile) : rows / tile + (a.E + 1) / 2) * parts_of(cols, tile);
+    };
     const int64_t large = tiles(256), rounds = parts_of(large, 256);
-    if (large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1};
-    return {tiles(128) >= 256 ? 128 : 64, 1};
+    if (large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1, 2};
+    const int64_t mid = tiles(128), small = tiles(64);
+    if (mid < 256 && small <= 768) return {64, 1, small <= 512 ? 4 : 3};
+    return {128, 1, mid <= 256 && !input ? 3 : 2};
 }
 
 // Weight gradients.  256 where there are two rounds of it and its edges waste no more than 128's would; else 128, or 64
@@ -712,12 +748,12 @@ Cut cut_rows(const ExpertArgs &a, int cols) {
 // rows of 16 experts of 512 x 512 46 / 46, 32768 rows of 2 of 128 x 128 81 / 19, of 128 x 127 786 / 43.
 Cut cut_weight(const ExpertArgs &a) {
     auto tiles = [&](int64_t tile) { return a.E * parts_of(a.N, tile) * parts_of(a.K, tile); };
-    if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1};
+    if (tiles(256) >= 512 && tiles(256) * 4 * 20 <= tiles(128) * 23) return {256, 1, 2};
     const int64_t steps = parts_of((int64_t)a.T * a.k, (int64_t)a.E * kDeep);
     auto cut = [&](int tile) {
         int64_t parts = parts_of(512, tiles(tile));
         if (parts > steps / 8) parts = steps / 8;
-        return Cut{tile, (int)(parts < 1 ? 1 : parts)};
+        return Cut{tile, (int)(parts < 1 ? 1 : parts), 2};
     };
     const Cut c = cut(128);
     return tiles(128) * c.parts >= 256 ? c : cut(64);
@@ -729,7 +765,7 @@ bool chunks(const ExpertArgs &a) {
            (!a.gy || aligned16(a.gy)) && aligned16(a.out) && aligned16(a.out32);
 }
 
-template <int MODE, int TILE, int WM, int WN, bool STAGED = false>
+template <int MODE, int TILE, int WM, int WN, bool STAGED = false, int BUFFERS = 2>
 hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
     const int64_t tiles = MODE == kWeight ? a.E * parts_of(a.N, TILE) * parts_of(a.K, TILE) * a.parts
                                           : most_row_tiles(a, TILE) * parts_of(MODE == kForward ? a.N : a.K, TILE);
@@ -746,9 +782,9 @@ hipError_t launch_tile(const ExpertArgs &a, hipStream_t st) {
         } else {
             if (a.tokens && kGathers)
                 return (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32)
-                           ? go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, kGathers, false>)
-                           : go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, false, false>);
-            return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false, false>);
+                           ? go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, kGathers, false, BUFFERS>)
+                           : go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, kGathers, false, false, BUFFERS>);
+            return go(sk_experts_tile<T, MODE, TILE, TILE, WM, WN, false, false, false, BUFFERS>);
         }
     });
 }
@@ -767,17 +803,17 @@ hipError_t launch_few(const ExpertArgs &a, hipStream_t st) {
 }
 
 // Rows in 8 bits, which are whole chunks always.
-template <int TILE, int WM, int WN>
+template <int TILE, int WM, int WN, int BUFFERS = 2>
 hipError_t launch_pairs(const ExpertArgs &a, hipStream_t st) {
     const int64_t tiles = most_row_tiles(a, TILE) * parts_of(a.N, TILE);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)(parts_of(tiles, 8) * 8)), dim3(WM * WN * 64), 0, st, a);
         return hipGetLastError();
     };
-    if (!a.tokens) return go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, false, false, false>);
+    if (!a.tokens) return go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, false, false, false, BUFFERS>);
     return (int64_t)a.T * a.K * 2 >= (int64_t(1) << 32)
-               ? go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, true, false>)
-               : go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, false, false>);
+               ? go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, true, false, BUFFERS>)
+               : go(sk_experts_tile<Pair, kForward, TILE, TILE, WM, WN, true, false, false, BUFFERS>);
 }
 
 template <int MODE>
@@ -785,12 +821,20 @@ hipError_t launch_product(const ExpertArgs &a, const Cut &c, hipStream_t st) {
     if (!chunks(a))
         return c.tile == 64 ? launch_tile<MODE, 64, 2, 2, true>(a, st) : launch_tile<MODE, 128, 2, 2, true>(a, st);
     if (c.tile == 256) return launch_tile<MODE, 256, 2, 4>(a, st);
-    if (c.tile == 128) return launch_tile<MODE, 128, 2, 2>(a, st);
-    return launch_tile<MODE, 64, 2, 2>(a, st);
+    if constexpr (MODE != kWeight) {
+        if (c.tile == 64)
+            return c.buffers == 4 ? launch_tile<MODE, 64, 2, 2, false, 4>(a, st) : launch_tile<MODE, 64, 2, 2, false, 3>(a, st);
+    } else if (c.tile == 64) {
+        return launch_tile<MODE, 64, 2, 2>(a, st);
+    }
+    if constexpr (MODE == kForward) {
+        if (c.buffers == 3) return launch_tile<MODE, 128, 2, 2, false, 3>(a, st);
+    }
+    return launch_tile<MODE, 128, 2, 2>(a, st);
 }
 
 hipError_t launch_rows_input(const ExpertArgs &a, hipStream_t st) {
-    return launch_product<kInput>(a, cut_rows(a, a.K), st);
+    return launch_product<kInput>(a, cut_rows(a, true), st);
 }
 
 }  // namespace
@@ -810,18 +854,17 @@ hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     // Only large matrices have tiles enough then: 32 rows of 8192 x 8192 57 / 90, but 64 rows 98 / 93.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
-    return launch_product<kForward>(a, cut_rows(a, a.N), st);
+    return launch_product<kForward>(a, cut_rows(a, false), st);
 }
 
 hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
     ExpertArgs a = p;
     a.whole_out = aligned16(a.out) && (int64_t)a.N * (a.dtype == SK_F32 ? 4 : 2) % 16 == 0;
     a.out32 = a.dtype == SK_F32 ? static_cast<float *>(a.out) : nullptr;
-    // The rules of 16-bit rows.  Few / tiles here, in us: 64 rows of one of 2048 x 2048 6.1 / 7.2, of 4096 x 4096
-    // 14.5 / 17.3, of 8192 x 8192 52 / 49; 128 rows of one of 4096 x 4096 25 / 17; 256 rows of 64 of 2048 x 2048
-    // 51.5 / 51.5, 384 rows 56 / 52.
+    // Few / tiles, in us: 8 rows of one of 8192 x 8192 15.0 / 16.0, 16 16.7 / 16.1, 64 47 / 19; 16 rows of 4 of
+    // 2048 x 2048 6.2 / 6.3, 64 8.9 / 6.3; 64 rows of 64 of 1024 x 2048 17.9 / 19.3, 128 23.3 / 22.9; 512 33 / 28.
     const int64_t rows = (int64_t)a.T * a.k;
-    if (rows <= 64 || rows <= 4 * a.E) {
+    if (rows <= 8 || rows <= a.E) {
         const dim3 grid((unsigned)(parts_of(most_row_tiles(a, kFewRows) * parts_of(a.N, kFewCols), 8) * 8));
         if (a.tokens)
             hipLaunchKernelGGL((sk_experts_few<Pair, true>), grid, dim3(kThreads), 0, st, a);
@@ -829,10 +872,10 @@ hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
             hipLaunchKernelGGL((sk_experts_few<Pair, false>), grid, dim3(kThreads), 0, st, a);
         return hipGetLastError();
     }
-    const Cut c = cut_rows(a, a.N);
+    const Cut c = cut_rows(a, false);
     if (c.tile == 256) return launch_pairs<256, 2, 4>(a, st);
-    if (c.tile == 128) return launch_pairs<128, 2, 2>(a, st);
-    return launch_pairs<64, 2, 2>(a, st);
+    if (c.tile == 64) return c.buffers == 4 ? launch_pairs<64, 2, 2, 4>(a, st) : launch_pairs<64, 2, 2, 3>(a, st);
+    return c.buffers == 3 ? launch_pairs<128, 2, 2, 3>(a, st) : launch_pairs<128, 2, 2>(a, st);
 }
 
 hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {

@@ -167,6 +167,37 @@ def test_product(T, E, k, K, N, dtype, out):
     check_product(rows(T, K, 1, dtype), make(E, N, K, seed=2, by=K ** -0.5, dtype=BF16), offsets, tokens, out)
 
 
+# Tiles of 64 with four buffers and (from 513 on) three, and of 128 with three (from 769 of 64 on): contractions of no whole
+# step, one, and up to more than there are buffers.
+@pytest.mark.parametrize("K", [1, 96, 128, 129, 256, 300, 384, 400, 512, 513, 640, 777])
+@pytest.mark.parametrize("T,E,N", [(70, 2, 65), (2000, 1, 1400), (2000, 1, 1800)])
+def test_every_number_of_steps(T, E, N, K):
+    offsets, tokens, _ = routed(T, E, 1, K, none=0.05)
+    x, w = rows(T, K, 1, BF16), make(E, N, K, seed=2, by=K ** -0.5, dtype=BF16)
+    check_product(x, w, offsets, tokens, F32)
+    check_product(x, w, torch.tensor([0, *[T // 2] * (E - 1), T - 3], dtype=torch.int32).cuda(), None, packed=True)
+
+
+@pytest.mark.parametrize("K", [8, 64, 72, 128, 136, 192, 256, 320, 392])
+@pytest.mark.parametrize("T,E,N", [(70, 2, 72), (2000, 1, 1400), (2000, 1, 1800)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_every_number_of_steps_in_16_bits(T, E, N, K, dtype):
+    """The product forward, and the input gradient with K as its contraction (N a row's columns)."""
+    offsets, tokens, slots = routed(T, E, 1, K, none=0.05)
+    x, w = make(T, K, seed=1, dtype=dtype), make(E, N, K, seed=2, by=K ** -0.5, dtype=dtype)
+    p = products(x.cpu(), w.cpu(), offsets.cpu(), tokens.cpu())
+    y = sk.sinkhorn_expert_product(x, w, offsets, tokens, slots)
+    far = (y.cpu().double() - p["y"]).abs()
+    assert bool((far <= rounding(p["y"], dtype) + 2 * (K + 8) * U * p["abs_y"]).all())
+    back, v, gy = w.mT.contiguous(), make(T, N, seed=3, dtype=dtype).requires_grad_(), x  # [E, K, N]
+    o = offsets.clone()
+    o[-1] = T - 5
+    p = products(v.detach().cpu(), back.cpu(), o.cpu(), None, gy.cpu())
+    gx, = torch.autograd.grad(sk.sinkhorn_expert_product(v, back, o), v, gy)
+    far = (gx.cpu().double() - p["gx"]).abs()
+    assert bool((far <= rounding(p["gx"], dtype) + 2 * (K + 8) * U * p["abs_gx"]).all())
+
+
 @pytest.mark.parametrize("T,E,K,N", [(5, 3, 40, 24), (300, 4, 200, 130), (3000, 2, 256, 2048)])
 def test_product_of_rows_in_order(T, E, K, N):
     offsets = torch.tensor([0] + sorted(torch.randint(0, T, (E,), generator=gen(3)).tolist()), dtype=torch.int32).cuda()
