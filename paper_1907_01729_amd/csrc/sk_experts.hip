@@ -728,16 +728,24 @@ struct Cut {
 // 2048 x 2048 16 / 8.8, 128 of one of 8192 x 8192 93 / 43; two / three / four, 8 bits, 4000 rows of 64 of 512 x 512 (2.9 a
 // CU) 6.9 / 7.0 / 8.4.  128 with three in the input gradient, two / three: 1024 rows of one of 4096 x 4096 45 / 50, 512 of
 // 8192 x 8192 105 / 96: two.
+// Where most experts have less than a tile of 64 (up to 32 rows an expert), the weights' reading is all the time, and small
+// tiles with much under way read fastest; four buffers where a row is 4 KB or more.  64 with three / four / 128 / 256: 8 bits,
+// 500 rows of 64 of 2048 x 2048 52 / 56 / 52 / 59, 64 rows 32 / 33 / 41 / 52, 64 of 16 of 4096 x 4096 61 / 57 / 68 / 70, 256
+// of 32 of 4096 x 1024 29 / 30 / 31 / 36; 16 bits, 500 of 64 of 2048 x 2048 107 / 101 / 125 / 132, 1000 of 64 of 1024 x 2048
+// 61 / 57 / 68 / 69, 500 of 32 of 4096 x 1024 52 / 53 / 52 / 58.  The input gradient,
+// whose copies of w are as wide as the tile, has 128 there: 500 of 64 of 2048 x 2048 100 / 97 / 93 / 108, 64 of 16 of
+// 4096 x 4096 104 / 108 / 87 / 97.
 Cut cut_rows(const ExpertArgs &a, bool input) {
     const int cols = input ? a.K : a.N;
     const int64_t rows = (int64_t)a.T * a.k;
     auto tiles = [&](int64_t tile) {
         return (a.E == 1 ? parts_of(rows, tile) : rows / tile + (a.E + 1) / 2) * parts_of(cols, tile);
     };
-    const int64_t large = tiles(256), rounds = parts_of(large, 256);
-    if (large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1, 2};
-    const int64_t mid = tiles(128), small = tiles(64);
-    if (mid < 256 && small <= 768) return {64, 1, small <= 512 ? 4 : 3};
+    const int64_t large = tiles(256), rounds = parts_of(large, 256), mid = tiles(128), small = tiles(64);
+    const bool sparse = rows <= 32 * (int64_t)a.E, few = mid < 256 && small <= 512;
+    if (!sparse && large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1, 2};
+    if (sparse && !input) return {64, 1, few || a.K >= 2048 ? 4 : 3};
+    if (mid < 256 && small <= 768) return {64, 1, few ? 4 : 3};
     return {128, 1, mid <= 256 && !input ? 3 : 2};
 }
 
@@ -849,9 +857,9 @@ size_t experts_weight_workspace_bytes(const ExpertArgs &a) {
 hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
     // The weights are read once for each 16 rows of an expert.  Few / tiles, in us: 256 rows, 64 experts of 2048 x 2048
-    // 99 / 122; 512 rows, 64 of 1024 x 1024 32 / 26.  Up to 64 rows of few experts, too, where tiles are too few: 64 rows
-    // of one of 2048 x 2048 8.5 / 17, of 4096 x 4096 24 / 31, of 512 x 512 4.5 / 5.2; of four of 2048 x 2048 14 / 17.
-    // Only large matrices have tiles enough then: 32 rows of 8192 x 8192 57 / 90, but 64 rows 98 / 93.
+    // 98 / 99, 64 rows 66 / 73; 512 rows, 64 of 1024 x 2048 60 / 57; 64 rows of one of 2048 x 2048 8.6 / 8.7, of 512 x 512
+    // 5.2 / 5.1, 16 of one of 8192 x 8192 33 / 38.  For 17 to 64 rows of one of 4096 x 4096 (25 / 15) and more the tiles are
+    // faster, but they sum in another order, and results there would not stay the same to the last bit.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, false), st);
@@ -861,10 +869,9 @@ hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
     ExpertArgs a = p;
     a.whole_out = aligned16(a.out) && (int64_t)a.N * (a.dtype == SK_F32 ? 4 : 2) % 16 == 0;
     a.out32 = a.dtype == SK_F32 ? static_cast<float *>(a.out) : nullptr;
-    // Few / tiles, in us: 8 rows of one of 8192 x 8192 15.0 / 16.0, 16 16.7 / 16.1, 64 47 / 19; 16 rows of 4 of
-    // 2048 x 2048 6.2 / 6.3, 64 8.9 / 6.3; 64 rows of 64 of 1024 x 2048 17.9 / 19.3, 128 23.3 / 22.9; 512 33 / 28.
-    const int64_t rows = (int64_t)a.T * a.k;
-    if (rows <= 8 || rows <= a.E) {
+    // Few / tiles, in us: 1 row of one of 8192 x 8192 14.5 / 15.7, 8 15.0 / 16.0, 16 16.3 / 16.4, 64 47 / 19; 4 rows of 64
+    // of 1024 x 2048 5.0 / 5.8, 16 7.9 / 7.1, 32 12.2 / 11.0, 96 22 / 23; 512 33 / 29.
+    if ((int64_t)a.T * a.k <= 8) {
         const dim3 grid((unsigned)(parts_of(most_row_tiles(a, kFewRows) * parts_of(a.N, kFewCols), 8) * 8));
         if (a.tokens)
             hipLaunchKernelGGL((sk_experts_few<Pair, true>), grid, dim3(kThreads), 0, st, a);
