@@ -554,7 +554,8 @@ __global__ __launch_bounds__(WM *WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 // many wavefronts have to ask for them at once.  A work-group takes kFewCols columns, and its four wavefronts a quarter
 // of the contraction each, straight from memory to registers; their sums meet in LDS.  A lane's 32 bytes of a row's 128
 // are two fragments: the products' order along the contraction is free as long as both factors have the same.  16 rows
-// of 14 of 64 experts of 1024 x 2048: 59 MB in 13 us (4.5 TB/s); in tiles of 64 18 us.  In 8 bits: 30 MB in 9 us.
+// of 14 of 64 experts of 1024 x 2048: 59 MB in 12.5 us (4.7 TB/s), in tiles of 64 with four buffers 11.0; in 8 bits 7.9
+// and 7.2.
 
 constexpr int kFewRows = 16, kFewCols = 32, kFewChunk = 64, kFewAtOnce = 4;
 
@@ -858,8 +859,9 @@ hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
     // The weights are read once for each 16 rows of an expert.  Few / tiles, in us: 256 rows, 64 experts of 2048 x 2048
     // 98 / 99, 64 rows 66 / 73; 512 rows, 64 of 1024 x 2048 60 / 57; 64 rows of one of 2048 x 2048 8.6 / 8.7, of 512 x 512
-    // 5.2 / 5.1, 16 of one of 8192 x 8192 33 / 38.  For 17 to 64 rows of one of 4096 x 4096 (25 / 15) and more the tiles are
-    // faster, but they sum in another order, and results there would not stay the same to the last bit.
+    // 5.2 / 5.1, 16 of one of 8192 x 8192 33 / 38; 16 rows of 64 of 1024 x 2048 12.5 / 11.0.  For 17 to 64 rows of one of
+    // 4096 x 4096 (25 / 15) and more the tiles are much faster, but they sum in another order, and results there would not
+    // stay the same to the last bit.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
     return launch_product<kForward>(a, cut_rows(a, false), st);

@@ -121,6 +121,11 @@ __device__ __forceinline__ void load_kept(const PackArgs &A, int64_t row, int c,
 }
 
 // ---- activations ----
+//
+// The activated rows are rounded to 16 bits, since the products' matrix instructions take such factors, and so is their
+// gradient between the product and the activation's derivative: each adds an error of the size of the result's own rounding
+// (bf16: 0.0024 of the norm in all, against 0.0017).  That gradient in 32 bits would cost 134 MB more, 27 of 600 us, for
+// 32768 rows of 1024.
 
 // exp(x): off by one unit of the hardware's power of two and by |x| units for its argument's rounding.
 __device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }

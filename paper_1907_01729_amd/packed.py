@@ -68,7 +68,7 @@ def sinkhorn_activation(x, activation, gated=False):
 def sinkhorn_expert_product_kept(x, weight, offsets, tokens=None, slots=None, activation="none", gated=False):
     """As sinkhorn_expert_product, of the activated rows act(x) (as sinkhorn_activation; x has 2 K columns where gated),
     with x kept in 8 bits for the backward pass instead of 16, a scale for each 128 columns of a row; the activated rows
-    are not kept.  The result is of x as given; the gradients take x at the values kept, activated again and rounded to
-    x's type."""
+    are not kept.  The result is of x as given, its activated rows rounded to x's type; the gradients take x at the values
+    kept, activated again and rounded to x's type."""
     return load_torch_library().product_kept(x, weight, offsets, tokens, slots, _ACTIVATIONS.get(activation, -1),
                                              bool(gated))
