@@ -160,6 +160,14 @@ std::shared_ptr<N> new_node(A &&...a) {
     return std::shared_ptr<N>(new N(std::forward<A>(a)...), torch::autograd::deleteNode);
 }
 SavedVariable keep(const Tensor &t) { return SavedVariable(t, false); }
+// What a node kept, in the layout that the kernels take: hooks on saved tensors may give the same values back with other
+// strides, and at another address.
+Tensor restored(const SavedVariable &v) { return contiguous(v.unpack()); }
+// Of what the node allocated itself, which begins at whole 16 bytes.
+Tensor restored_own(const SavedVariable &v) {
+    const Tensor t = restored(v);
+    return t.defined() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 ? t.clone() : t;
+}
 
 // ---- norms ----
 
@@ -200,7 +208,7 @@ struct NormNode : Node {
 
     variable_list gradients(const variable_list &grads) override {
         if (!grads[0].defined()) return variable_list(3);
-        const Tensor xv = x.unpack(), wv = w.unpack(), bv = b.unpack(), sv = stats.unpack();
+        const Tensor xv = restored(x), wv = restored(w), bv = restored(b), sv = restored_own(stats);
         const On on(xv);
         const Tensor gx = wants(0) ? at::empty_like(xv) : Tensor(),
                      gw = wv.defined() && wants(1) ? at::empty_like(wv) : Tensor(),
@@ -260,9 +268,9 @@ struct ResidualNode : Node {
     variable_list gradients(const variable_list &grads) override {
         const Tensor g_out = grads[0], g_next = grads.size() > 1 ? grads[1] : Tensor();
         if (!g_out.defined() && !g_next.defined()) return variable_list(7);
-        const Tensor hv = h.unpack(), gv = gate.unpack(), awv = aw.unpack(), abv = ab.unpack(), bwv = bw.unpack(),
-                     bbv = bb.unpack(), sv = stats.unpack();
-        const Tensor ov = has_out ? out.unpack(shared_from_this()) : Tensor();
+        const Tensor hv = restored(h), gv = restored(gate), awv = restored(aw), abv = restored(ab), bwv = restored(bw),
+                     bbv = restored(bb), sv = restored_own(stats);
+        const Tensor ov = has_out ? contiguous(out.unpack(shared_from_this())) : Tensor();
         const On on(sv);
         auto made = [&](size_t i, const Tensor &as) {
             return as.defined() && wants(i) ? at::empty_like(as) : Tensor();
@@ -590,7 +598,7 @@ struct KeptRows {
     int64_t columns = 0;
     KeptRows() = default;
     explicit KeptRows(const Packed &p) : values(keep(p.values)), scales(keep(p.scales)), columns(p.columns) {}
-    Packed unpack() const { return {values.unpack(), scales.unpack(), columns, kKeptBlock}; }
+    Packed unpack() const { return {restored_own(values), restored_own(scales), columns, kKeptBlock}; }
     void release() { values.reset_data(), scales.reset_data(); }
 };
 
@@ -644,7 +652,7 @@ struct KeptNode : Node {
 
     variable_list gradients(const variable_list &grads) override {
         if (!grads[0].defined()) return variable_list(2);
-        const Tensor w = weight.unpack(), off = offsets.unpack(), tok = tokens.unpack(), sl = slots.unpack();
+        const Tensor w = restored(weight), off = restored(offsets), tok = restored(tokens), sl = restored(slots);
         const Packed kept = rows.unpack();
         const Tensor &gy = grads[0];
         const On on(w);
