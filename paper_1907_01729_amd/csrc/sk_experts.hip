@@ -736,14 +736,19 @@ struct Cut {
 // 61 / 57 / 68 / 69, 500 of 32 of 4096 x 1024 52 / 53 / 52 / 58.  The input gradient,
 // whose copies of w are as wide as the tile, has 128 there: 500 of 64 of 2048 x 2048 100 / 97 / 93 / 108, 64 of 16 of
 // 4096 x 4096 104 / 108 / 87 / 97.
-Cut cut_rows(const ExpertArgs &a, bool input) {
+// Rows that are no whole chunks have two buffers, in tiles of 64 or 128: 64 where the larger ones do not go round, and
+// forward where experts have few rows.  64 / 128, in us: forward, 500 rows of 64 of 1003 x 1001 31 / 34, 1000 of them
+// 37 / 34, 1000 of 64 of 2050 x 517 37 / 56, 256 of 32 of 1999 x 2041 62 / 58; input gradient, 1780 of 4 of 1021 x 2041
+// 34 / 51, 2700 of 16 of 2045 x 1017 64 / 92.
+Cut cut_rows(const ExpertArgs &a, bool input, bool whole) {
     const int cols = input ? a.K : a.N;
-    const int64_t rows = (int64_t)a.T * a.k;
+    const int64_t rows = (int64_t)a.T * a.k, half = (a.E + 1) / 2;
     auto tiles = [&](int64_t tile) {
-        return (a.E == 1 ? parts_of(rows, tile) : rows / tile + (a.E + 1) / 2) * parts_of(cols, tile);
+        return (a.E == 1 ? parts_of(rows, tile) : rows / tile + half) * parts_of(cols, tile);
     };
     const int64_t large = tiles(256), rounds = parts_of(large, 256), mid = tiles(128), small = tiles(64);
     const bool sparse = rows <= 32 * (int64_t)a.E, few = mid < 256 && small <= 512;
+    if (!whole) return {mid < 256 || (sparse && !input) ? 64 : 128, 1, 2};
     if (!sparse && large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1, 2};
     if (sparse && !input) return {64, 1, few || a.K >= 2048 ? 4 : 3};
     if (mid < 256 && small <= 768) return {64, 1, few ? 4 : 3};
@@ -843,7 +848,7 @@ hipError_t launch_product(const ExpertArgs &a, const Cut &c, hipStream_t st) {
 }
 
 hipError_t launch_rows_input(const ExpertArgs &a, hipStream_t st) {
-    return launch_product<kInput>(a, cut_rows(a, true), st);
+    return launch_product<kInput>(a, cut_rows(a, true, chunks(a)), st);
 }
 
 }  // namespace
@@ -864,7 +869,7 @@ hipError_t launch_experts_forward(const ExpertArgs &a, hipStream_t st) {
     // stay the same to the last bit.
     const int64_t rows = (int64_t)a.T * a.k;
     if (chunks(a) && (rows <= 64 || rows <= 4 * a.E)) return launch_few(a, st);
-    return launch_product<kForward>(a, cut_rows(a, false), st);
+    return launch_product<kForward>(a, cut_rows(a, false, chunks(a)), st);
 }
 
 hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
@@ -881,7 +886,7 @@ hipError_t launch_experts_packed(const ExpertArgs &p, hipStream_t st) {
             hipLaunchKernelGGL((sk_experts_few<Pair, false>), grid, dim3(kThreads), 0, st, a);
         return hipGetLastError();
     }
-    const Cut c = cut_rows(a, false);
+    const Cut c = cut_rows(a, false, true);
     if (c.tile == 256) return launch_pairs<256, 2, 4>(a, st);
     if (c.tile == 64) return c.buffers == 4 ? launch_pairs<64, 2, 2, 4>(a, st) : launch_pairs<64, 2, 2, 3>(a, st);
     return c.buffers == 3 ? launch_pairs<128, 2, 2, 3>(a, st) : launch_pairs<128, 2, 2>(a, st);
