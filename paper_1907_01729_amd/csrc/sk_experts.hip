@@ -718,7 +718,9 @@ struct Cut {
 // work-group a CU; wherever its last round is filled it halves what the tiles read.  128: two a CU, which cover each
 // other's first copies and last writes, or one with another step of copies under way.  64: too few tiles of 128 to go
 // round.  What is under way bounds those, so they have as many buffers as let all tiles run at once: four up to two a CU,
-// three up to three.
+// three up to three.  128 with three has a CU to itself, so one tile past 256 doubles its time: it is taken where there are
+// no more whatever the shares (a last tile for each expert).  1760 rows of 16 of 1536 x 2048, 288 tiles, with two 26 us,
+// with three 43; 1648 of 8 of 2048 x 512, 272 tiles, 11.5 / 16.3, in 8 bits 8.3 / 12.1.
 // Measured, 256 / 128 / 64, in us: 65536 rows of 64 experts of 2048 x 2048 (9.0 rounds) 535 / 611 / 916; 8192 rows of 8 of
 // 4096 x 2048 (2.3 rounds) 161 / 159 / 223; 8000 rows of 2 of 2048 x 1024 (1.0) 32 / 39 / 53.  Equal shares of whole tiles
 // come out even better in 256 (8192 rows of 8: 118 / 147), but how the shares are is known on the device alone.
@@ -743,16 +745,16 @@ struct Cut {
 Cut cut_rows(const ExpertArgs &a, bool input, bool whole) {
     const int cols = input ? a.K : a.N;
     const int64_t rows = (int64_t)a.T * a.k, half = (a.E + 1) / 2;
-    auto tiles = [&](int64_t tile) {
-        return (a.E == 1 ? parts_of(rows, tile) : rows / tile + half) * parts_of(cols, tile);
+    auto tiles = [&](int64_t tile, int64_t last) {
+        return (a.E == 1 ? parts_of(rows, tile) : rows / tile + last) * parts_of(cols, tile);
     };
-    const int64_t large = tiles(256), rounds = parts_of(large, 256), mid = tiles(128), small = tiles(64);
+    const int64_t large = tiles(256, half), rounds = parts_of(large, 256), mid = tiles(128, half), small = tiles(64, half);
     const bool sparse = rows <= 32 * (int64_t)a.E, few = mid < 256 && small <= 512;
     if (!whole) return {mid < 256 || (sparse && !input) ? 64 : 128, 1, 2};
     if (!sparse && large >= 256 && large * 20 >= rounds * 256 * 17) return {256, 1, 2};
     if (sparse && !input) return {64, 1, few || a.K >= 2048 ? 4 : 3};
     if (mid < 256 && small <= 768) return {64, 1, few ? 4 : 3};
-    return {128, 1, mid <= 256 && !input ? 3 : 2};
+    return {128, 1, tiles(128, a.E) <= 256 && !input ? 3 : 2};
 }
 
 // Weight gradients.  256 where there are two rounds of it and its edges waste no more than 128's would; else 128, or 64
