@@ -427,6 +427,10 @@ SK_API size_t sinkhorn_experts_workspace_bytes(const sk_experts *p);
 SK_API sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_y, const void *w,
                                                  const int32_t *offsets, const int32_t *slots, void *grad_x,
                                                  void *workspace, size_t ws_bytes, void *stream);
+/* The same in fp32, not rounded: for what multiplies it further before it is. */
+SK_API sk_status sinkhorn_experts_backward_input32(const sk_experts *p, const void *grad_y, const void *w,
+                                                   const int32_t *offsets, const int32_t *slots, float *grad_x,
+                                                   void *workspace, size_t ws_bytes, void *stream);
 
 /*
  * Gradient of w [E, N, K]: sum_r grad_y[r]^T x[src(r)] over each expert's rows
@@ -583,6 +587,10 @@ SK_API sk_status sinkhorn_activation_forward(const sk_packing *p, int32_t activa
 SK_API sk_status sinkhorn_activation_backward(const sk_packing *p, int32_t activation, int32_t gated,
                                               const void *values, const float *scales, const void *grad_y, void *y,
                                               void *grad_x, void *stream);
+/* The same with grad_y in fp32. */
+SK_API sk_status sinkhorn_activation_backward32(const sk_packing *p, int32_t activation, int32_t gated,
+                                                const void *values, const float *scales, const float *grad_y, void *y,
+                                                void *grad_x, void *stream);
 
 /*
  * Experts' products of rows in 8 bits: as sinkhorn_experts_forward with

@@ -49,6 +49,7 @@ EXPORTED = (
     "sinkhorn_experts_backward_input",
     "sinkhorn_experts_weight_workspace_bytes",
     "sinkhorn_experts_backward_weight",
+    "sinkhorn_experts_backward_input32",
     "sinkhorn_dropout",
     "sinkhorn_combine_forward",
     "sinkhorn_combine_backward",
@@ -61,6 +62,7 @@ EXPORTED = (
     "sinkhorn_unpack",
     "sinkhorn_activation_forward",
     "sinkhorn_activation_backward",
+    "sinkhorn_activation_backward32",
     "sinkhorn_experts_forward_packed",
 )
 
@@ -159,6 +161,7 @@ def load_library():
     lib.sinkhorn_experts_workspace_bytes.argtypes = [PE]
     lib.sinkhorn_experts_workspace_bytes.restype = Z
     lib.sinkhorn_experts_backward_input.argtypes = [PE, P, P, P, P, P, P, Z, P]
+    lib.sinkhorn_experts_backward_input32.argtypes = [PE, P, P, P, P, P, P, Z, P]
     lib.sinkhorn_experts_weight_workspace_bytes.argtypes = [PE]
     lib.sinkhorn_experts_weight_workspace_bytes.restype = Z
     lib.sinkhorn_experts_backward_weight.argtypes = [PE, P, P, P, P, P, P, Z, P]
@@ -176,11 +179,13 @@ def load_library():
     lib.sinkhorn_unpack.argtypes = [PK, *[P] * 4]
     lib.sinkhorn_activation_forward.argtypes = [PK, I, I, *[P] * 5]
     lib.sinkhorn_activation_backward.argtypes = [PK, I, I, *[P] * 6]
+    lib.sinkhorn_activation_backward32.argtypes = [PK, I, I, *[P] * 6]
     lib.sinkhorn_experts_forward_packed.argtypes = [PE, *[P] * 8]
     for name in ("route_forward", "route_backward", "experts_forward", "experts_backward_input",
-                 "experts_backward_weight", "dropout", "combine_forward", "combine_backward", "norm_forward",
+                 "experts_backward_input32", "experts_backward_weight", "dropout", "combine_forward", "combine_backward", "norm_forward",
                  "norm_backward", "residual_norm_forward", "residual_norm_backward", "pack", "unpack",
-                 "activation_forward", "activation_backward", "experts_forward_packed"):
+                 "activation_forward", "activation_backward", "activation_backward32",
+                 "experts_forward_packed"):
         getattr(lib, "sinkhorn_" + name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -227,8 +227,9 @@ sk_status sinkhorn_activation_forward(const sk_packing *p, int32_t activation, i
     return status_of(sk::launch_activation_forward(a, static_cast<hipStream_t>(stream)));
 }
 
-sk_status sinkhorn_activation_backward(const sk_packing *p, int32_t activation, int32_t gated, const void *values,
-                                       const float *scales, const void *grad_y, void *y, void *grad_x, void *stream) {
+static sk_status activation_backward(const sk_packing *p, int32_t activation, int32_t gated, const void *values,
+                                     const float *scales, const void *grad_y, bool gy32, void *y, void *grad_x,
+                                     void *stream) {
     const sk_status st = check_activation(p, activation, gated, true);
     if (st != SK_OK) return st;
     if (p->rows == 0 || (!y && !grad_x)) return SK_OK;
@@ -240,9 +241,20 @@ sk_status sinkhorn_activation_backward(const sk_packing *p, int32_t activation, 
     a.values = static_cast<int8_t *>(const_cast<void *>(values));
     a.scales = const_cast<float *>(scales);
     a.gy = grad_y;
+    a.gy32 = gy32;
     a.y = y;
     a.gx = grad_x;
     return status_of(sk::launch_activation_backward(a, static_cast<hipStream_t>(stream)));
+}
+
+sk_status sinkhorn_activation_backward(const sk_packing *p, int32_t activation, int32_t gated, const void *values,
+                                       const float *scales, const void *grad_y, void *y, void *grad_x, void *stream) {
+    return activation_backward(p, activation, gated, values, scales, grad_y, false, y, grad_x, stream);
+}
+
+sk_status sinkhorn_activation_backward32(const sk_packing *p, int32_t activation, int32_t gated, const void *values,
+                                         const float *scales, const float *grad_y, void *y, void *grad_x, void *stream) {
+    return activation_backward(p, activation, gated, values, scales, grad_y, true, y, grad_x, stream);
 }
 
 sk_status sinkhorn_experts_forward_packed(const sk_experts *p, const void *xv, const float *xs, const void *wv,

@@ -214,13 +214,13 @@ size_t sinkhorn_experts_workspace_bytes(const sk_experts *p) {
     return sk::experts_workspace_bytes(p->T, p->k, p->K);
 }
 
-sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_y, const void *w,
-                                          const int32_t *offsets, const int32_t *slots, void *grad_x,
-                                          void *workspace, size_t ws_bytes, void *stream) {
+static sk_status backward_input(const sk_experts *p, const void *grad_y, const void *w, const int32_t *offsets,
+                                const int32_t *slots, void *grad_x, float *grad_x32, void *workspace, size_t ws_bytes,
+                                void *stream) {
     const sk_status st = check_experts(p);
     if (st != SK_OK) return st;
     if (p->T == 0) return SK_OK;
-    if (!grad_y || !w || !offsets || !grad_x) return SK_ERR_NULLPTR;
+    if (!grad_y || !w || !offsets || (!grad_x && !grad_x32)) return SK_ERR_NULLPTR;
     if (slots) {
         if (ws_bytes < sk::experts_workspace_bytes(p->T, p->k, p->K)) return SK_ERR_WORKSPACE;
         if (!workspace) return SK_ERR_NULLPTR;
@@ -231,7 +231,20 @@ sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_
     a.offsets = offsets;
     a.slots = slots;
     a.out = grad_x;
+    a.out32 = grad_x32;
     return status_of(sk::launch_experts_input(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+sk_status sinkhorn_experts_backward_input(const sk_experts *p, const void *grad_y, const void *w,
+                                          const int32_t *offsets, const int32_t *slots, void *grad_x,
+                                          void *workspace, size_t ws_bytes, void *stream) {
+    return backward_input(p, grad_y, w, offsets, slots, grad_x, nullptr, workspace, ws_bytes, stream);
+}
+
+sk_status sinkhorn_experts_backward_input32(const sk_experts *p, const void *grad_y, const void *w,
+                                            const int32_t *offsets, const int32_t *slots, float *grad_x,
+                                            void *workspace, size_t ws_bytes, void *stream) {
+    return backward_input(p, grad_y, w, offsets, slots, nullptr, grad_x, workspace, ws_bytes, stream);
 }
 
 size_t sinkhorn_experts_weight_workspace_bytes(const sk_experts *p) {

@@ -645,7 +645,7 @@ __global__ __launch_bounds__(kThreads) void sk_experts_few(ExpertArgs A) {
 
 // gx[t] = sum over the token's slots of the rows' gradients, kept in 32 bits until here; eight columns to a thread.
 // Memory: 65536 rows of 2048 in 118 us (5.1 TB/s).
-template <class T>
+template <class T>  // the result's
 __global__ __launch_bounds__(kThreads) void sk_experts_sum_slots(ExpertArgs A, const float *rows, T *gx) {
     const int64_t chunks = (A.K + 7) / 8, all = (int64_t)A.T * A.k;
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -901,13 +901,14 @@ hipError_t launch_experts_input(const ExpertArgs &a, void *ws, hipStream_t st) {
     r.out32 = static_cast<float *>(ws);
     const hipError_t e = launch_rows_input(r, st);
     if (e != hipSuccess) return e;
-    return with_half(a.dtype, [&](auto type) {
-        using T = decltype(type);
+    auto sum = [&](auto *to) {
+        using T = std::remove_pointer_t<decltype(to)>;
         const dim3 grid((unsigned)parts_of((int64_t)a.T * parts_of(a.K, 8), kThreads));
-        hipLaunchKernelGGL((sk_experts_sum_slots<T>), grid, dim3(kThreads), 0, st, a, static_cast<const float *>(ws),
-                           static_cast<T *>(a.out));
+        hipLaunchKernelGGL((sk_experts_sum_slots<T>), grid, dim3(kThreads), 0, st, a, static_cast<const float *>(ws), to);
         return hipGetLastError();
-    });
+    };
+    if (a.out32) return sum(a.out32);
+    return with_half(a.dtype, [&](auto type) { return sum(static_cast<decltype(type) *>(a.out)); });
 }
 
 hipError_t launch_experts_weight(const ExpertArgs &a, void *ws, hipStream_t st) {

@@ -15,6 +15,7 @@ struct PackArgs {
     int64_t rows;
     int columns, pitch, blocks;  // blocks: scales of a row
     int dtype, kind, gated;
+    int gy32;  // gy is in 32 bits, whatever dtype is
     int lanes;
 };
 inline int pack_pitch(int columns) { return (columns + 15) / 16 * 16; }

@@ -122,10 +122,11 @@ __device__ __forceinline__ void load_kept(const PackArgs &A, int64_t row, int c,
 
 // ---- activations ----
 //
-// The activated rows are rounded to 16 bits, since the products' matrix instructions take such factors, and so is their
-// gradient between the product and the activation's derivative: each adds an error of the size of the result's own rounding
-// (bf16: 0.0024 of the norm in all, against 0.0017).  That gradient in 32 bits would cost 134 MB more, 27 of 600 us, for
-// 32768 rows of 1024.
+// The activated rows are rounded to 16 bits, since the products' matrix instructions take such factors, and so is in bf16
+// their gradient between the product and the activation's derivative: each adds an error of the size of the result's own
+// rounding (0.0023 of the norm in all, against 0.0017).  That gradient in 32 bits costs 134 MB more, 22 of 659 us, for 32768
+// rows of 1024.  In fp16, whose range would lose numbers there, it is kept so (the gradient's type is a parameter of its
+// own).
 
 // exp(x): off by one unit of the hardware's power of two and by |x| units for its argument's rounding.
 __device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void sk_unpack(PackArgs A) {
     store_left(static_cast<T *>(A.y) + p.row * A.columns + p.c, p.left, v);
 }
 
-template <class T, bool GATED>
+template <class T, class G, bool GATED>  // G: the type of gy
 __global__ __launch_bounds__(kThreads) void sk_activation_backward(PackArgs A) {
     const int cols = GATED ? A.columns / 2 : A.columns;
     const Place p = place_of(A.rows, cols);
@@ -295,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void sk_activation_backward(PackArgs A) {
     float v[8], u[8], g[8], y[8], d[8];
     load_kept(A, p.row, p.c, p.left, v);
     if (GATED) load_kept(A, p.row, cols + p.c, p.left, u);
-    if (A.gx) load_left(static_cast<const T *>(A.gy) + p.row * cols + p.c, p.left, g);
+    if (A.gx) load_left(static_cast<const G *>(A.gy) + p.row * cols + p.c, p.left, g);
     activate8(A.kind, v, y, d);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -385,11 +386,12 @@ hipError_t launch_activation_backward(const PackArgs &a, hipStream_t st) {
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
         const dim3 grid = grid_of(a.rows * ((cols + 7) / 8));
-        if (a.gated)
-            hipLaunchKernelGGL((sk_activation_backward<T, true>), grid, dim3(kThreads), 0, st, a);
-        else
-            hipLaunchKernelGGL((sk_activation_backward<T, false>), grid, dim3(kThreads), 0, st, a);
-        return hipGetLastError();
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a);
+            return hipGetLastError();
+        };
+        if (a.gy32) return a.gated ? go(sk_activation_backward<T, float, true>) : go(sk_activation_backward<T, float, false>);
+        return a.gated ? go(sk_activation_backward<T, T, true>) : go(sk_activation_backward<T, T, false>);
     });
 }
 

@@ -584,10 +584,14 @@ std::pair<Tensor, Tensor> activate_backward(const Packed &kept, int64_t kind, bo
     shape.back() = kept.columns;
     const Tensor y = wants_y ? empty(activated_shape(kept.values.sizes(), kept.columns, gated), kept.values, type) : Tensor();
     const Tensor gx = gy.defined() ? empty(shape, kept.values, type) : Tensor();
+    const bool wide = gy.defined() && gy.scalar_type() != type;  // gy in 32 bits
     const sk_packing p =
         packing(row_count(kept.values.sizes().slice(0, kept.values.dim() - 1)), kept.columns, kKeptBlock, type);
-    check(sinkhorn_activation_backward(&p, static_cast<int32_t>(kind), gated, data(kept.values),
-                                       data_of<float>(kept.scales), data(gy), data(y), data(gx), on.stream),
+    check(wide ? sinkhorn_activation_backward32(&p, static_cast<int32_t>(kind), gated, data(kept.values),
+                                                data_of<float>(kept.scales), data_of<float>(gy), data(y), data(gx),
+                                                on.stream)
+               : sinkhorn_activation_backward(&p, static_cast<int32_t>(kind), gated, data(kept.values),
+                                              data_of<float>(kept.scales), data(gy), data(y), data(gx), on.stream),
           "sinkhorn_activation_backward");
     return {y, gx};
 }
@@ -658,12 +662,20 @@ struct KeptNode : Node {
         const On on(w);
         Tensor gx, a, gw;
         if (wants(0)) {
-            gx = empty({sl.defined() ? p.T : static_cast<int64_t>(p.T) * p.k, p.K}, w, type);
+            // What an activation's derivative and the other half still multiply stays in 32 bits in float16, whose range
+            // would lose a gradient (past 65504, or below 3e-8) that these bring back into it.  bfloat16 has the range.
+            const bool wide = (kind || gated) && type == at::kHalf;
+            gx = empty({sl.defined() ? p.T : static_cast<int64_t>(p.T) * p.k, p.K}, w, wide ? at::kFloat : type);
             const size_t need = sl.defined() ? sinkhorn_experts_workspace_bytes(&p) : 0;
             const Tensor ws = empty_bytes(need, w);
-            check(sinkhorn_experts_backward_input(&p, data(gy), data(w), data_of<int32_t>(off), data_of<int32_t>(sl),
-                                                  data(gx), data(ws), need, on.stream),
-                  "sinkhorn_experts_backward_input");
+            const auto run = [&](auto entry, auto *to) {
+                check(entry(&p, data(gy), data(w), data_of<int32_t>(off), data_of<int32_t>(sl), to, data(ws), need, on.stream),
+                      "sinkhorn_experts_backward_input");
+            };
+            if (wide)
+                run(sinkhorn_experts_backward_input32, data_of<float>(gx));
+            else
+                run(sinkhorn_experts_backward_input, data(gx));
         }
         if (kind || gated)
             std::tie(a, gx) = activate_backward(kept, kind, gated, type, gx, wants(1), on);

@@ -68,7 +68,9 @@ def sinkhorn_activation(x, activation, gated=False):
 def sinkhorn_expert_product_kept(x, weight, offsets, tokens=None, slots=None, activation="none", gated=False):
     """As sinkhorn_expert_product, of the activated rows act(x) (as sinkhorn_activation; x has 2 K columns where gated),
     with x kept in 8 bits for the backward pass instead of 16, a scale for each 128 columns of a row; the activated rows
-    are not kept.  The result is of x as given, its activated rows rounded to x's type; the gradients take x at the values
-    kept, activated again and rounded to x's type."""
+    are not kept.  The result is of x as given, its activated rows rounded to x's type (in float16 one past 65504 is
+    infinite); the gradients take x at the values kept, activated again and rounded to x's type.  Between the product and
+    the activation's derivative the rows' gradient is rounded to bfloat16, too; in float16, which has not the range for it,
+    it stays in 32 bits there."""
     return load_torch_library().product_kept(x, weight, offsets, tokens, slots, _ACTIVATIONS.get(activation, -1),
                                              bool(gated))
