@@ -128,22 +128,30 @@ __device__ __forceinline__ void load_kept(const PackArgs &A, int64_t row, int c,
 // rows of 1024.  In fp16, whose range would lose numbers there, it is kept so (the gradient's type is a parameter of its
 // own).
 
-// exp(x): off by one unit of the hardware's power of two and by |x| units for its argument's rounding.
-__device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
+// exp(x) and 1 / x for rows of type T.  In 16-bit rows by the hardware's power of two, off by one of its units and by |x|
+// for its argument's rounding, and its reciprocal, off by one: far below their own rounding.
+template <class T>
+__device__ __forceinline__ float exp_of(float x) {
+    return sizeof(T) == 4 ? expf(x) : ex2(x * kLog2e);
+}
+template <class T>
+__device__ __forceinline__ float inverse_of(float x) {
+    return sizeof(T) == 4 ? 1.f / x : __builtin_amdgcn_rcpf(x);
+}
 
 // act(x), and its derivative in d.
-template <int KIND>
+template <class T, int KIND>
 __device__ __forceinline__ float activate(float x, float &d) {
     if constexpr (KIND == SK_ACT_RELU) {
         d = x > 0.f ? 1.f : 0.f;
         return x > 0.f ? x : x != x ? x : 0.f;
     } else if constexpr (KIND == SK_ACT_SILU) {
-        const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-x));
+        const float p = inverse_of<T>(1.f + exp_of<T>(-x));
         d = p * (1.f + x * (1.f - p));
         return x * p;
     } else if constexpr (KIND == SK_ACT_GELU) {
         const float p = 0.5f * erfcf(x * -0.70710678118654752f);  // (1 + erf) / 2 without its cancellation
-        d = p + x * exp_of(-0.5f * x * x) * 0.39894228040143268f;
+        d = p + x * exp_of<T>(-0.5f * x * x) * 0.39894228040143268f;
         return x * p;
     } else {
         d = 1.f;
@@ -151,10 +159,11 @@ __device__ __forceinline__ float activate(float x, float &d) {
     }
 }
 // Of eight numbers; one choice for all of them.
+template <class T>
 __device__ __forceinline__ void activate8(int kind, const float (&x)[8], float (&y)[8], float (&d)[8]) {
     auto all = [&](auto k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = activate<decltype(k)::value>(x[i], d[i]);
+        for (int i = 0; i < 8; ++i) y[i] = activate<T, decltype(k)::value>(x[i], d[i]);
     };
     if (kind == SK_ACT_RELU)
         all(std::integral_constant<int, SK_ACT_RELU>{});
@@ -238,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void sk_pack_blocks(PackArgs A) {
     }
     if constexpr (ACT) {
         float y[8], d[8];
-        activate8(A.kind, x[0], y, d);
+        activate8<T>(A.kind, x[0], y, d);
         if constexpr (GATED) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] *= x[1][j];
@@ -270,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void sk_activation(PackArgs A) {
     const T *x = static_cast<const T *>(A.x) + p.row * A.columns + p.c;
     float v[8], u[8], y[8], d[8];
     load_left(x, p.left, v);
-    activate8(A.kind, v, y, d);
+    activate8<T>(A.kind, v, y, d);
     if (GATED) {
         load_left(x + cols, p.left, u);
 #pragma unroll
@@ -297,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void sk_activation_backward(PackArgs A) {
     load_kept(A, p.row, p.c, p.left, v);
     if (GATED) load_kept(A, p.row, cols + p.c, p.left, u);
     if (A.gx) load_left(static_cast<const G *>(A.gy) + p.row * cols + p.c, p.left, g);
-    activate8(A.kind, v, y, d);
+    activate8<T>(A.kind, v, y, d);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (A.gx) v[j] = g[j] * d[j] * (GATED ? u[j] : 1.f);
