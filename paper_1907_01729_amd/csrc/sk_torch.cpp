@@ -3,6 +3,7 @@
 // norm with its gradients takes the host 45 us a step, with a node written in Python 105.
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/VariableTypeUtils.h>
@@ -10,6 +11,7 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/saved_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <mutex>
@@ -97,6 +99,13 @@ struct On {
 
 // ---- autograd ----
 
+// torch.jit.trace and make_fx record torch's own operations alone: of a call of these its allocations, whose memory a
+// replay would give out as nobody wrote it.
+void not_traced(const char *what) {
+    using Mode = c10::impl::TorchDispatchModeKey;
+    TORCH_CHECK_NOT_IMPLEMENTED(!torch::jit::tracer::isTracing() && !c10::impl::TorchDispatchModeTLS::get_mode(Mode::PROXY),
+                                what, " cannot be traced");
+}
 // These have no derivative in forward mode, and a result without one would pass for zero.
 void no_tangent(const char *what, std::initializer_list<Tensor> inputs) {
     for (const Tensor &t : inputs)
@@ -133,6 +142,7 @@ struct Node : torch::autograd::Node {
 
     variable_list apply(variable_list &&grads) override {
         const std::lock_guard<std::mutex> lock(mutex_);  // two backward passes through one graph
+        not_traced(what);
         check_capture();
         const bool again = at::GradMode::is_enabled();
         for (const Tensor &g : grads) no_tangent(what, {g});
@@ -227,6 +237,7 @@ struct NormNode : Node {
 };
 
 Tensor norm(const Tensor &x_, const NormOf &norm_) {
+    not_traced("sinkhorn_norm");
     const Tensor x = contiguous(x_);
     const Norm n = norm_of(norm_);
     rows(x, "x");
@@ -299,9 +310,10 @@ struct ResidualNode : Node {
 
 variable_list residual_norm(const Tensor &h_, const Tensor &residual_, const Maybe &gate_, double scale,
                             const std::optional<NormOf> &after_, const std::optional<NormOf> &before_) {
+    const char *what = "sinkhorn_residual_norm";
+    not_traced(what);
     const Tensor h = contiguous(h_), residual = contiguous(residual_), gate = contiguous(or_none(gate_));
     const Norm after = after_ ? norm_of(*after_) : Norm{}, before = before_ ? norm_of(*before_) : Norm{};
-    const char *what = "sinkhorn_residual_norm";
     rows(h, "h");
     like(residual, "residual", h, h.scalar_type());
     shaped(residual, "residual", h.sizes());
@@ -423,6 +435,7 @@ Packed packed_of(const PackedOf &given, const std::string &name, bool by_rows) {
 }
 
 std::pair<Tensor, Tensor> pack(const Tensor &x_, int64_t block) {
+    not_traced("sinkhorn_pack");
     at::AutoGradMode off(false);
     const Tensor x = contiguous(x_);
     columns_of(x, "x");
@@ -447,6 +460,7 @@ void result_type(at::ScalarType type) {
     TORCH_CHECK_TYPE(type_of(type) >= 0, "dtype must be float32, bfloat16 or float16, got ", type);
 }
 Tensor unpack(const PackedOf &packed, at::ScalarType type) {
+    not_traced("sinkhorn_unpack");
     at::AutoGradMode off(false);
     const Packed p = packed_of(packed, "packed", false);
     result_type(type);
@@ -487,6 +501,7 @@ struct Constant : torch::autograd::Node {
 
 Tensor product_packed(const Maybe &x_, const std::optional<PackedOf> &packed_, const PackedOf &weight_,
                       const Maybe &offsets_, const Maybe &tokens_, const std::optional<at::ScalarType> &type_) {
+    not_traced("sinkhorn_expert_product_packed");
     const Packed weight = packed_of(weight_, "weight", true);
     const Tensor offsets = or_none(offsets_), tokens = or_none(tokens_);
     const int64_t dims = weight.values.dim();
@@ -625,6 +640,7 @@ struct ActivationNode : Node {
 };
 
 Tensor activation(const Tensor &x_, int64_t kind, bool gated) {
+    not_traced("sinkhorn_activation");
     const Tensor x = contiguous(x_);
     columns_of(x, "x");
     activation_of(kind, gated, x.size(-1));
@@ -700,8 +716,9 @@ struct KeptNode : Node {
 
 Tensor product_kept(const Tensor &x_, const Tensor &weight_, const Tensor &offsets, const Maybe &tokens_,
                     const Maybe &slots_, int64_t kind, bool gated) {
-    const Tensor tokens = or_none(tokens_), slots = or_none(slots_);
     const char *what = "sinkhorn_expert_product_kept";
+    not_traced(what);
+    const Tensor tokens = or_none(tokens_), slots = or_none(slots_);
     TORCH_CHECK_VALUE(tokens.defined() == slots.defined(), "tokens and slots go together");
     const Tensor x = contiguous(x_), weight = contiguous(weight_);
     typed(weight, "weight", true);

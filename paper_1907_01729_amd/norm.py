@@ -47,6 +47,20 @@ def _norms(T, N, dtype, wdtype, gate, gdtype, after, before, scale, eps_after, e
     return ref, int(load_library().sinkhorn_norm_workspace_bytes(ref))
 
 
+_PROXY = torch._C._TorchDispatchModeKey.PROXY
+
+
+def _not_traced(fn):
+    """Refuses fn within torch.jit.trace and make_fx, which record its allocations alone: a replay would give out memory
+    that nobody wrote."""
+    @functools.wraps(fn)
+    def call(*args, **kwargs):
+        if torch._C._is_tracing() or torch._C._get_dispatch_mode(_PROXY) is not None:
+            raise NotImplementedError(f"{fn.__name__} cannot be traced")
+        return fn(*args, **kwargs)
+    return call
+
+
 def _rows(x, name):
     _typed(x, name)
     if x.dim() != 2:
@@ -112,6 +126,7 @@ def _norm_sizes(x, norm):
 
 
 @_on_stream
+@_not_traced
 def sinkhorn_norm_forward(x, norm=Norm()):
     """(norm of x [T, N], stats); stats goes to sinkhorn_norm_backward.  stream=: as in sinkhorn_forward."""
     sizes = _norm_sizes(x, norm)
@@ -122,6 +137,7 @@ def sinkhorn_norm_forward(x, norm=Norm()):
 
 
 @_on_stream
+@_not_traced
 def sinkhorn_norm_backward(x, norm, stats, grad_y, workspace=None):
     """(grad_x, grad_weight, grad_bias) from the norm's gradient; None for what the norm does not have."""
     sizes = _norm_sizes(x, norm)
@@ -152,6 +168,7 @@ def _residual_sizes(h, gate, scale, after, before):
 
 
 @_on_stream
+@_not_traced
 def sinkhorn_residual_norm_forward(h, residual, gate=None, scale=1.0, after=None, before=None):
     """(out, next, stats) of a block's end: see sinkhorn_residual_norm; stats goes to
     sinkhorn_residual_norm_backward.  stream=: as in sinkhorn_forward."""
@@ -166,6 +183,7 @@ def sinkhorn_residual_norm_forward(h, residual, gate=None, scale=1.0, after=None
 
 
 @_on_stream
+@_not_traced
 def sinkhorn_residual_norm_backward(h, out, stats, grad_out=None, grad_next=None, gate=None, scale=1.0, after=None,
                                     before=None, workspace=None):
     """NormGradients from those of out and next (each may be None)."""
