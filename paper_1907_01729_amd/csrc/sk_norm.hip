@@ -374,7 +374,7 @@ __global__ __launch_bounds__(THREADS, GATE || (END && sizeof(T) == 4) ? 2 : 4) v
             if ((before || WIDE) && mine) {  // WIDE: zeros are written, too
                 float xd[8], yd[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) yd[i] = (float)v.dy[i], xd[i] = yd[i] * xh(i);
+                for (int i = 0; i < 8; ++i) yd[i] = (float)v.dy[i], xd[i] = before ? yd[i] * xh(i) : 0.f;
                 add(Array<kBeforeW>{}, w, xd);
                 add(Array<kBeforeB>{}, w, yd);
             }
