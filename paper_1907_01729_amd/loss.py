@@ -34,10 +34,10 @@ class SinkhornLoss(torch.autograd.Function):
             if want_C:
                 raise NotImplementedError("the sharp gradient is taken with respect to mu and nu only")
             g = sinkhorn_backward_sharp(grad_loss.contiguous(), mu.contiguous(), nu.contiguous(), C.contiguous(),
-                                        ctx.lam, alpha, beta)
+                                        ctx.lam, alpha.contiguous(), beta.contiguous())
             return g["grad_mu"], g["grad_nu"], None, None, None, None, None, None
         g = sinkhorn_backward(grad_loss.contiguous(), mu.contiguous(), nu.contiguous(), C.contiguous(), ctx.lam,
-                              alpha, beta, grad_C=want_C)
+                              alpha.contiguous(), beta.contiguous(), grad_C=want_C)
         gC = None
         if want_C:
             gC = g["grad_C"].reshape(C.shape) if C.dim() == 3 or g["grad_C"].shape[0] == 1 else g["grad_C"]
@@ -78,7 +78,7 @@ class SinkhornPointsLoss(torch.autograd.Function):
             grad_loss = mu.new_zeros(mu.shape[0])
         want = ctx.needs_input_grad[2] or ctx.needs_input_grad[3]
         g = sinkhorn_backward_points(grad_loss.contiguous(), mu.contiguous(), nu.contiguous(), X.contiguous(),
-                                     Y.contiguous(), ctx.lam, alpha, beta, grad_points=want)
+                                     Y.contiguous(), ctx.lam, alpha.contiguous(), beta.contiguous(), grad_points=want)
         gX = g["grad_X"].reshape(X.shape) if want and ctx.needs_input_grad[2] else None
         gY = g["grad_Y"].reshape(Y.shape) if want and ctx.needs_input_grad[3] else None
         return g["grad_mu"], g["grad_nu"], gX, gY, None, None, None

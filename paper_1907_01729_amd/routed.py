@@ -223,6 +223,11 @@ def _contiguous(g):
     return None if g is None else g.contiguous()
 
 
+def _saved(ctx):
+    """The saved tensors, dense: hooks on them may give the same values back with other strides."""
+    return map(_contiguous, ctx.saved_tensors)
+
+
 class _Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, bias, mask, renormalize):
@@ -236,7 +241,7 @@ class _Route(torch.autograd.Function):
     @staticmethod
     @_first_order
     def backward(ctx, g_weights, _e, _c, _o, _t, _s, g_balance, g_z):
-        logits, weights, experts, counts, state = ctx.saved_tensors
+        logits, weights, experts, counts, state = _saved(ctx)
         return _route_backward(logits, ctx.k, weights, experts, counts, state, _contiguous(g_weights),
                                _contiguous(g_balance), _contiguous(g_z), ctx.renormalize), None, None, None, None
 
@@ -388,7 +393,7 @@ class _ExpertProduct(torch.autograd.Function):
     @staticmethod
     @_first_order
     def backward(ctx, gy):
-        x, weight, offsets, tokens, slots = ctx.saved_tensors
+        x, weight, offsets, tokens, slots = _saved(ctx)
         gy, need_x, need_w = gy.contiguous(), *ctx.needs_input_grad[:2]
         gx = _run_experts_input(gy, weight, offsets, slots, ctx.sizes) if need_x else None
         gw = _run_experts_weight(gy, x, offsets, tokens, ctx.sizes) if need_w else None
@@ -513,7 +518,7 @@ class _Combine(torch.autograd.Function):
     @staticmethod
     @_first_order
     def backward(ctx, gy):
-        z, weights, slots, offsets = ctx.saved_tensors
+        z, weights, slots, offsets = _saved(ctx)
         gz = gw = None
         if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
             gz, gw = _run_combine_backward(z, weights, slots, offsets, gy.contiguous(), *ctx.call)
