@@ -88,8 +88,9 @@ def _forward_mode():
 def _recorded(*inputs):
     """Whether a call goes through autograd: where a gradient of an input is wanted, and in forward mode, where autograd
     refuses an input with a tangent (the operators have no such derivative, and a result without one would pass for
-    zero).  A call that goes past it saves ten microseconds."""
-    if _forward_mode():
+    zero), and within torch.jit.trace, which keeps an autograd function, but of a call past it the allocations alone.  A
+    call that goes past it saves ten microseconds."""
+    if _forward_mode() or torch._C._is_tracing():
         return True
     if torch.is_grad_enabled():
         for t in inputs:
@@ -314,7 +315,7 @@ def _experts_sizes(x, weight, offsets, tokens, halves=1):
         _match(tokens, "tokens", x, None, torch.int32)
         T = x.shape[0]
         k = _rows_of(tokens.numel(), T, "tokens")
-    return T, k, E, K, N, _HALF[x.dtype]
+    return *map(int, (T, k, E, K, N)), _HALF[x.dtype]  # torch.jit.trace gives out sizes as tensors
 
 
 def _run_experts(x, weight, offsets, tokens, sizes):
@@ -465,7 +466,7 @@ def _combine_sizes(z, weights, slots):
         raise ValueError(f"z must be [T k, D] and slots [T, k], got {list(z.shape)} {list(slots.shape)}")
     _match(weights, "weights", z, slots.shape, torch.float32)
     T, k = slots.shape
-    return T, z.shape[1], max(k, 1) if T == 0 else k
+    return tuple(map(int, (T, z.shape[1], max(k, 1) if T == 0 else k)))
 
 
 @_on_stream
