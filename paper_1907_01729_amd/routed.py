@@ -304,10 +304,9 @@ def sinkhorn_experts_forward(x, weight, offsets, tokens=None):
     return _run_experts(x, weight, offsets, tokens, _experts_sizes(x, weight, offsets, tokens))
 
 
-def _experts_sizes(x, weight, offsets, tokens, halves=1):
-    """halves: 2 where x's rows are twice as wide as the product's."""
+def _experts_sizes(x, weight, offsets, tokens):
     E, N, K = _weight(weight)
-    _half_rows(x, "x", halves * K, weight)
+    _half_rows(x, "x", K, weight)
     _match(offsets, "offsets", x, (E + 1,), torch.int32)
     if tokens is None:
         T, k = _rows_in_order(x.shape[0])
