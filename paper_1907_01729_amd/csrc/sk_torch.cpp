@@ -502,6 +502,7 @@ struct Constant : torch::autograd::Node {
 Tensor product_packed(const Maybe &x_, const std::optional<PackedOf> &packed_, const PackedOf &weight_,
                       const Maybe &offsets_, const Maybe &tokens_, const std::optional<at::ScalarType> &type_) {
     not_traced("sinkhorn_expert_product_packed");
+    TORCH_CHECK_TYPE(x_ || packed_, "x must be a GPU tensor or a Packed");
     const Packed weight = packed_of(weight_, "weight", true);
     const Tensor offsets = or_none(offsets_), tokens = or_none(tokens_);
     const int64_t dims = weight.values.dim();
