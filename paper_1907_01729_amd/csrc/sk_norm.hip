@@ -371,10 +371,10 @@ __global__ __launch_bounds__(THREADS, GATE || (END && sizeof(T) == 4) ? 2 : 4) v
         float d[8], q[3] = {0.f, 0.f, 0.f};
         each([&](const Window &w) {
             gradient(d);
-            if ((before || WIDE) && mine) {  // WIDE: zeros are written, too
+            if (before && mine) {
                 float xd[8], yd[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) yd[i] = (float)v.dy[i], xd[i] = before ? yd[i] * xh(i) : 0.f;
+                for (int i = 0; i < 8; ++i) yd[i] = (float)v.dy[i], xd[i] = yd[i] * xh(i);
                 add(Array<kBeforeW>{}, w, xd);
                 add(Array<kBeforeB>{}, w, yd);
             }
@@ -466,7 +466,7 @@ constexpr int kSumThreads = 256, kSumColumns = 16;
 struct SumArgs {
     const float *parts;
     void *to[kArrays];
-    int f32[kArrays];
+    int f32[kArrays], from[kArrays];  // from: its place among the parts' arrays; -1: none, its sum is zero
     int blocks, arrays, N;
 };
 
@@ -474,12 +474,12 @@ template <class T>
 __global__ __launch_bounds__(kSumThreads) void sk_norm_sums(SumArgs A) {
     constexpr int kLanes = kSumColumns / 4, kRuns = kSumThreads / kLanes;
     __shared__ float4 part[kRuns][kLanes];
-    const int lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes, array = blockIdx.y;
+    const int lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes, array = blockIdx.y, place = A.from[array];
     const int c = blockIdx.x * kSumColumns + lane * 4, left = A.N - c;
-    const int each = (A.blocks + kRuns - 1) / kRuns, end = min(A.blocks, (run + 1) * each);
+    const int blocks = place < 0 ? 0 : A.blocks, each = (blocks + kRuns - 1) / kRuns, end = min(blocks, (run + 1) * each);
     float4 s = {0.f, 0.f, 0.f, 0.f};
     for (int b = run * each; b < end; ++b) {
-        const float *from = A.parts + ((int64_t)b * A.arrays + array) * A.N + c;
+        const float *from = A.parts + ((int64_t)b * A.arrays + place) * A.N + c;
         if (left >= 4) {
             float4 v;
             __builtin_memcpy(&v, from, 16);
@@ -545,14 +545,16 @@ hipError_t launch_norm_backward(NormArgs a, void *ws, hipStream_t st) {
     a.lanes = row_lanes(a.N, kMostLanes);
     a.parts = static_cast<float *>(ws);
     SumArgs s = {};
+    int outputs = 0;
     void *const wanted[kArrays] = {a.g_after_w, a.g_before_w, a.g_after_b, a.g_before_b,
                                    a.gate_kind == SK_GATE_COLUMNS ? a.g_gate : nullptr};
     for (int i = 0; i < kArrays; ++i) {
         a.place[i] = -1;
         if (!wanted[i]) continue;
-        s.to[a.arrays] = wanted[i];
-        s.f32[a.arrays] = i == kGate ? a.gf32 : a.wf32;
-        a.place[i] = a.arrays++;
+        s.to[outputs] = wanted[i];
+        s.f32[outputs] = i == kGate ? a.gf32 : a.wf32;
+        if (a.g_next || (i != kBeforeW && i != kBeforeB)) a.place[i] = a.arrays++;
+        s.from[outputs++] = a.place[i];
     }
     const bool bias = a.g_after_b || a.g_before_b, gate = a.gate_kind > SK_GATE_ROWS;
     s.parts = a.parts;
@@ -584,8 +586,8 @@ hipError_t launch_norm_backward(NormArgs a, void *ws, hipStream_t st) {
             return threads == 512 ? by_sums(std::false_type{}, end, half) : by_sums(std::false_type{}, end, full);
         };
         const hipError_t e = a.T == 0 ? hipSuccess : a.end ? by_size(std::true_type{}) : by_size(std::false_type{});
-        if (e != hipSuccess || !a.arrays) return e;
-        hipLaunchKernelGGL((sk_norm_sums<T>), dim3((unsigned)((a.N + kSumColumns - 1) / kSumColumns), a.arrays),
+        if (e != hipSuccess || !outputs) return e;
+        hipLaunchKernelGGL((sk_norm_sums<T>), dim3((unsigned)((a.N + kSumColumns - 1) / kSumColumns), outputs),
                            dim3(kSumThreads), 0, st, s);
         return hipGetLastError();
     });
