@@ -236,11 +236,11 @@ enum { kAfterW, kBeforeW, kAfterB, kBeforeB, kGate, kArrays };
 template <int A>
 using Array = std::integral_constant<int, A>;
 
-// A work-group's groups go through rows, the next row's loads under way while a row is worked on (without that the block's
-// end of 65536 x 2048 took 434 us, with it 266).  The sums over the
-// rows stay in registers and are added up over the groups at the end, into one part a work-group; WIDE: rows of more
-// windows than lanes, whose sums lie in the work-group's own part of memory and which are read again from the caches for
-// each pass over them.  BIAS: there are sums for biases; GATE: the gate is more than a number a row.  Without them fewer
+// A work-group's groups go through rows, the next row's loads under way while a row is worked on (65536 x 2048, bf16,
+// without / with that, in us: the norm's gradients 197 / 161, a block's end with two norms 359 / 332, with the next norm
+// alone and one gradient for both 224 / 223).  The sums over the rows stay in registers and are added up over the groups
+// at the end, into one part a work-group; WIDE: rows of more windows than lanes, whose sums lie in the work-group's own
+// part of memory and which are read again from the caches for each pass over them.  BIAS: there are sums for biases; GATE: the gate is more than a number a row.  Without them fewer
 // registers are taken: two work-groups of 512 threads fit on a CU with up to 128 (16-bit rows, no such gate).  Of 1024
 // threads one does; where its registers do not hold the next row, too, that is loaded when it is its turn.
 template <class T, bool WIDE, bool END, bool BIAS, bool GATE, int THREADS>
