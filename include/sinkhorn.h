@@ -574,8 +574,8 @@ SK_API sk_status sinkhorn_unpack(const sk_packing *p, const void *values, const 
  *   y = act(x) [rows, columns],  or with gated = 1
  *   y = act(x[:, :K]) x[:, K:]   [rows, K],  columns = 2 K,
  * act(x) = x, max(x, 0), x / (1 + exp(-x)), x (1 + erf(x / sqrt 2)) / 2.  In 32
- * bits, one rounding to dtype.  values and scales (p->block = 128; both or none)
- * receive x in 8 bits, as in sinkhorn_pack.
+ * bits, one rounding to dtype (fp16: infinite past 65504).  values and scales
+ * (p->block = 128; both or none) receive x in 8 bits, as in sinkhorn_pack.
  */
 typedef enum { SK_ACT_NONE = 0, SK_ACT_RELU = 1, SK_ACT_SILU = 2, SK_ACT_GELU = 3 } sk_activation;
 SK_API sk_status sinkhorn_activation_forward(const sk_packing *p, int32_t activation, int32_t gated, const void *x,
